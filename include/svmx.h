@@ -28,7 +28,8 @@
  *    device holds at once, and (svm_train_static only) its static device scratch and that
  *    scratch's address on each device.
  *  - All device work is enqueued on options->stream (a hipStream_t; NULL = the null stream).
- *    Every call returns only after its outputs are complete.
+ *    Every call returns only after its outputs are complete, but for those under "Rows that are
+ *    learned from tokens", which only queue their work.
  *  - Negative status: nothing was written to the outputs that can be relied upon, nothing
  *    leaks; svm_last_error() explains.  SVM_NOT_CONVERGED (positive) means the iteration
  *    limit was reached: alpha is feasible (0 <= a <= C, sum a y = 0) and b is the current
@@ -287,6 +288,148 @@ svm_status svm_kernel_rows(const float *X, int64_t n, int64_t d, double gamma, c
 int64_t svm_gram_workspace_bytes(int64_t n, int64_t d, const svm_options *o);
 svm_status svm_gram(const float *X, int64_t n, int64_t d, double gamma, float *G, int64_t ld, void *workspace,
                     int64_t workspace_bytes, const svm_options *o);
+
+/*
+ * ---- Rows that are learned from tokens --------------------------------------------------------
+ *
+ * tokens -> svm_embed -> svm_layernorm -> X -> svm_train -> svm_objective_grad -> svm_layernorm_grad ->
+ * svm_embed_grad -> svm_adamw.  The operators before and behind a machine whose samples are token
+ * sequences, and the gradient that joins them: what the machine's objective loses or gains by a
+ * change of its rows.
+ *
+ * Other than the calls above, these are queued on options->stream and return without waiting (a
+ * training step is a dozen of them): outputs are complete in the order of that stream, buffers and
+ * workspaces must live until then, and a later failure on the device shows in a later call.  They
+ * read and write caller memory only, allocate nothing, and can be captured into a HIP graph.
+ * Rows are row-major with a pitch of ld values (ld >= d), at any alignment of their type; outputs
+ * must not overlap inputs unless a declaration says so.  Sums are fp32 or wider in an order that
+ * depends on the sizes alone (no atomics touch values), and each output is rounded once.
+ */
+
+/* Element types of the buffers below. */
+typedef enum {
+  SVM_F32 = 0,
+  SVM_BF16 = 1,
+  SVM_F16 = 2,
+  SVM_F8 = 3 /* e4m3 (largest value 448), optimiser states only */
+} svm_type;
+
+/*
+ * Embedding bags: out[b] = w_b * sum over the positions t of bag b of table[tokens[t]].
+ *   table   device [V][ld_table], SVM_F32, SVM_BF16 or SVM_F16
+ *   tokens  device int32 (token_bytes 4) or int64 (8) [T], each in 0..V-1 or equal to padding
+ *   bags    device int64 [B+1]: bag b is the positions bags[b] .. bags[b+1]-1 (bags[0] = 0,
+ *           bags[B] = T, none decreasing; an empty bag gives a row of zeros); or NULL: bag b is
+ *           position b, and B = T
+ *   scale   w_b = scale, or with mean != 0 scale / (the bag's tokens that are not padding)
+ *   padding tokens of this value add nothing, whatever the table holds there; negative: none
+ *   out     device [B][ld_out], SVM_F32, SVM_BF16 or SVM_F16, any of them for any table
+ *   invalid device int32 or NULL: set to 1 when a token or bags are not as said (left as it is
+ *           otherwise; one more launch).  Without it nothing outside the buffers is read or written
+ *           either: a token outside the table makes its row NaN (which a training then refuses),
+ *           and rows of bags that are not as said are undefined.
+ *   workspace  svm_embed_workspace_bytes (0 without bags; then it may be NULL)
+ * EINVAL: negative sizes, V or d < 1, sizes or pitches that overflow, T or B above 2^31 - 2, V or d
+ * above 2^31 - 2, a scale that is not finite, B != T without bags, NULL pointers, unknown types.
+ */
+int64_t svm_embed_workspace_bytes(int64_t T, int64_t d, int64_t B, int32_t has_bags);
+svm_status svm_embed(const void *table, int32_t table_type, int64_t V, int64_t d, int64_t ld_table, const void *tokens,
+                     int32_t token_bytes, int64_t T, const int64_t *bags, int64_t B, double scale, int32_t mean,
+                     int64_t padding, void *out, int32_t out_type, int64_t ld_out, int32_t *invalid, void *workspace,
+                     int64_t workspace_bytes, const svm_options *o);
+
+/*
+ * The gradient of svm_embed in the table: dE[v] = sum over the positions t with tokens[t] = v of
+ * w_b(t) dY[b(t)], positions in their order.  dY device [B][ld_dy] (any of the three types), dE device
+ * [V][ld_de] (any of the three).  accumulate = 0: every row of dE is written (zeros where no
+ * token points); otherwise the sums are added to what dE holds, and other rows are untouched.
+ * Padding and tokens outside the table get no gradient.  The other arguments as above.
+ */
+int64_t svm_embed_grad_workspace_bytes(int64_t T, int64_t d, int64_t B);
+svm_status svm_embed_grad(const void *tokens, int32_t token_bytes, int64_t T, const int64_t *bags, int64_t B,
+                          double scale, int32_t mean, int64_t padding, const void *dY, int32_t dy_type, int64_t ld_dy,
+                          void *dE, int32_t de_type, int64_t V, int64_t d, int64_t ld_de, int32_t accumulate,
+                          int32_t *invalid, void *workspace, int64_t workspace_bytes, const svm_options *o);
+
+/*
+ * Layer norm: mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) r weight + bias, row by row.
+ *   x       device [n][ld_x], SVM_F32, SVM_BF16 or SVM_F16
+ *   weight, bias  device [d] of weight_type (fp32 or x's type), or NULL (1 and 0)
+ *   y       device [n][ld_y], fp32 or x's type
+ *   mean, rstd  device fp32 [n] or NULL: mu and r, for the gradient
+ * EINVAL: n < 0, d < 1, eps not finite or <= 0, pitches below d, sizes that overflow, other types.
+ */
+svm_status svm_layernorm(const void *x, int32_t x_type, int64_t n, int64_t d, int64_t ld_x, const void *weight,
+                         const void *bias, int32_t weight_type, double eps, void *y, int32_t y_type, int64_t ld_y,
+                         float *mean, float *rstd, const svm_options *o);
+
+/*
+ * Its gradient: with h = (x - mu) r and q = dy weight, dx = r (q - mean(q) - h mean(q h)), dweight = sum
+ * over rows of dy h, dbias = sum over rows of dy (zeros for n = 0).
+ *   dy device [n][ld_dy], fp32 or x's type; dx device [n][ld_dx] of x's type; dweight, dbias device [d]
+ *   of weight_type, or NULL where not wanted; weight NULL: 1.
+ */
+int64_t svm_layernorm_grad_workspace_bytes(int64_t n, int64_t d, int32_t x_type);
+svm_status svm_layernorm_grad(const void *dy, int32_t dy_type, int64_t ld_dy, const void *x, int32_t x_type, int64_t n,
+                              int64_t d, int64_t ld_x, const float *mean, const float *rstd, const void *weight,
+                              int32_t weight_type, void *dx, int64_t ld_dx, void *dweight, void *dbias, void *workspace,
+                              int64_t workspace_bytes, const svm_options *o);
+
+/* One tensor of an AdamW step: `count` consecutive values. */
+typedef struct {
+  void *param;          /* SVM_F32, SVM_BF16 or SVM_F16, updated */
+  float *master;        /* fp32 copy that is updated in its place, param then being its rounding; or NULL */
+  const void *grad;     /* SVM_F32, SVM_BF16 or SVM_F16 */
+  void *m, *v;          /* states: fp32 [count], or e4m3 codes [count] */
+  float *m_scale, *v_scale; /* e4m3: device fp32 [ceil(count / 256)], value = code x scale of its 256; else NULL */
+  int64_t count;
+  double weight_decay;
+  int32_t param_type, grad_type;
+  int32_t state_type;   /* SVM_F32 or SVM_F8 */
+  int32_t reserved;     /* must be 0 */
+} svm_adamw_tensor;
+
+typedef struct {
+  int32_t struct_size;  /* = sizeof(svm_adamw_params) */
+  int32_t reserved;     /* must be 0 */
+  int64_t step;         /* 1 for the first step */
+  double lr, beta1, beta2, eps;
+  double grad_scale;    /* factor on every gradient (1: none) */
+  const float *grad_scale_device; /* device fp32: another factor, known on the device alone (clipping), or NULL */
+} svm_adamw_params;
+
+/*
+ * One AdamW step over `count` tensors (host array; read before the call returns), in place: g = scale grad,
+ * m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2, param = param (1 - lr weight_decay)
+ * - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps).  States start as zeros (codes and
+ * scales too).  e4m3 states: every block of 256 values is kept over its largest magnitude / 448, to
+ * nearest even, a second moment above 0 never as 0; a block below 2^-100 becomes zeros; a value that is
+ * not finite is kept as NaN and leaves its block's scale alone (the square of a finite gradient that
+ * overflows is kept as the largest fp32).  One launch for every 40 tensors.
+ * EINVAL: NULL pointers, unknown types, negative counts, step < 1, betas outside [0, 1), lr, eps, weight
+ * decay or grad_scale that are negative or not finite.
+ */
+svm_status svm_adamw(const svm_adamw_tensor *tensors, int64_t count, const svm_adamw_params *p, const svm_options *o);
+
+/*
+ * Gradient of decision values in their test samples: with c_j = alpha_j y_j,
+ * dX[q] = upstream[q] * 2 gamma sum_{a_j>0} c_j K(x_j, x_q) (x_j - x_q).
+ *   upstream device fp64 [m] or NULL (1), dX device fp32 [m][d]; the others as for svm_predict.
+ */
+int64_t svm_predict_grad_workspace_bytes(int64_t n, int64_t d, int64_t m);
+svm_status svm_predict_grad(const float *X_train, const int32_t *y, const double *alpha, int64_t n, int64_t d,
+                            double gamma, const float *X_test, int64_t m, const double *upstream, float *dX,
+                            void *workspace, int64_t workspace_bytes, const svm_options *o);
+
+/*
+ * Gradient of the machine's objective in its rows: W(a) of the solved dual equals the primal loss 1/2
+ * |w|^2 + C sum of hinge losses, and moves with the rows as W does at fixed a (the envelope theorem), so
+ * dX[i] = -c_i 2 gamma sum_j c_j K_ij (x_j - x_i): what to descend to make the classes easier to
+ * separate.  Rows that are no support vectors get zeros.
+ */
+int64_t svm_objective_grad_workspace_bytes(int64_t n, int64_t d);
+svm_status svm_objective_grad(const float *X, const int32_t *y, const double *alpha, int64_t n, int64_t d, double gamma,
+                              float *dX, void *workspace, int64_t workspace_bytes, const svm_options *o);
 
 /* Thread-local message for the last non-OK status of this thread ("" if none). */
 const char *svm_last_error(void);

@@ -20,16 +20,17 @@
 
 #include "common.hpp"
 #include "few_rule.hpp"
+#include "status.hpp"
 #include "warm.hpp"
 #include "svmx.h"
 
 using namespace svmx;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-svm_status fail(svm_status st, const char *fmt, ...) {
+svm_status svmx::fail(svm_status st, const char *fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -39,11 +40,9 @@ svm_status fail(svm_status st, const char *fmt, ...) {
   return st;
 }
 
-#define HIPCHK(expr)                                                                      \
-  do {                                                                                    \
-    hipError_t e_ = (expr);                                                               \
-    if (e_ != hipSuccess) return fail(SVM_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+void svmx::clear_error() { g_err.clear(); }
+
+namespace {
 
 constexpr int64_t DEFAULT_GRAM_BUDGET = 200LL << 30;  // bytes of HBM the Gram may take by default
 constexpr int32_t DEFAULT_CHECK_EVERY = 65536;
@@ -129,6 +128,17 @@ bool resolve(const svm_options *o, int64_t n, Opts *r) {
   return r->gram >= SVM_GRAM_AUTO && r->gram <= SVM_GRAM_OFF && r->levels >= 0 && r->levels <= 2 &&
          (r->gram_mfma == SVM_MFMA_SPLIT_F16 || r->gram_mfma == SVM_MFMA_F32) && ws_ok && r->resident_rows >= -1;
 }
+
+}  // namespace
+
+bool svmx::stream_of(const svm_options *o, hipStream_t *s) {
+  Opts r;
+  if (!resolve(o, 1, &r)) return false;
+  *s = r.stream;
+  return true;
+}
+
+namespace {
 
 // How a problem of n samples is spread over workgroups.
 struct Shape {

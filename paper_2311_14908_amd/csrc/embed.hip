@@ -1,0 +1,633 @@
+// embed.hip -- embedding bags and their gradient by sorted tokens.
+//
+// out_b = w_b sum over the positions t of bag b of E[token_t], w_b = scale or scale / (positions that
+// count); dE_v = sum over the positions t with token_t = v of w_b(t) dY_b(t).  Both are sums of rows over
+// runs: of positions with one bag, or, once the positions are sorted by token, of positions with one token.
+// Either way a run can be one position or all of them, so the work is cut by position, not by run: a
+// thread holds one unit (16 bytes of a row) of one chunk of consecutive positions, adds in fp32 in their
+// order, writes the runs that lie inside its chunk and leaves a partial sum where a run crosses an end;
+// a second kernel joins those.  No atomic touches a value, and each output is rounded once, so results
+// repeat bit for bit.
+#include "layers.hpp"
+#include "units.hpp"
+
+#include <type_traits>
+
+namespace svmx {
+
+namespace {
+
+constexpr int EB = 256;           // threads of a workgroup
+constexpr int EU = 8;             // rows of a thread on their way at once
+constexpr int64_t RANK_MAX = 8192;  // positions sorted by counting smaller ones
+constexpr int SORT_BLOCKS = 256;
+
+inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Positions of a chunk: about 2^18 threads of 8 values each, between 16 positions (below, the joins cost
+// more than the rows) and 128 (above, nothing is gained).
+int64_t chunk_of(int64_t T, int64_t d) {
+  const double want = (double)T * (double)div_up(d, 8) / 131072.0;
+  int64_t L = 16;
+  while (L < 128 && (double)L < want) L <<= 1;
+  return L;
+}
+
+__device__ __forceinline__ int64_t token_at(const EmbedCall &c, int64_t i) {
+  return c.wide ? static_cast<const int64_t *>(c.tokens)[i] : (int64_t)static_cast<const int32_t *>(c.tokens)[i];
+}
+
+// First b in [0, count) with a[b] >= x, or count.
+template <class I>
+__device__ __forceinline__ int64_t lower_bound(const I *__restrict__ a, int64_t count, I x) {
+  int64_t lo = 0, hi = count;
+  while (lo < hi) {
+    const int64_t mid = lo + ((hi - lo) >> 1);
+    if (a[mid] < x)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// The bag of position i (in range whatever the starts hold).
+__device__ __forceinline__ int64_t bag_at(const EmbedCall &c, int64_t i) {
+  if (!c.bags) return i;
+  const int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i + 1) - 1;
+  return b < 0 ? 0 : b >= c.B ? c.B - 1 : b;
+}
+
+// Item of this thread: `of` = which chunk or row, `unit` = which 16 bytes of it.
+__device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &unit) {
+  const int64_t b0 = (int64_t)blockIdx.x * EB, c0 = b0 / units;
+  const uint32_t r = (uint32_t)(b0 - c0 * units) + threadIdx.x;
+  of = c0 + r / (uint32_t)units;
+  unit = r % (uint32_t)units;
+}
+
+// Sum of E[token] over positions lo .. hi - 1, EU rows on their way at once; `used` counts positions that
+// are not padding.  A token outside the table reads nothing and makes the sum NaN.
+template <int N, class TE>
+__device__ __forceinline__ void sum_tokens(const EmbedCall &c, const TE *__restrict__ E, int64_t ld, int64_t lo, int64_t hi,
+                                           int64_t at, int64_t left, float (&acc)[N], int &used) {
+  for (int64_t i = lo; i < hi; i += EU) {
+    float v[EU][N];
+    bool live[EU], bad[EU];
+#pragma unroll
+    for (int q = 0; q < EU; ++q) {
+      const int64_t t = i + q < hi ? token_at(c, i + q) : 0;
+      live[q] = i + q < hi && (c.padding < 0 || t != c.padding);
+      bad[q] = live[q] && (t < 0 || t >= c.V);
+      load_n<N>(E + (live[q] && !bad[q] ? t : 0) * ld + at, left, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < EU; ++q) {
+      used += live[q] ? 1 : 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += bad[q] ? __builtin_nanf("") : live[q] ? v[q][e] : 0.f;
+    }
+  }
+}
+
+__device__ __forceinline__ float bag_weight(const EmbedCall &c, int64_t used) {
+  return c.mean ? c.scale / (float)(used > 0 ? used : 1) : c.scale;
+}
+
+// A row a position (no bags).
+template <int N, class TE>
+__global__ void __launch_bounds__(EB) embed_rows_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
+                                                   int32_t out_type, int64_t ld_out, int64_t units) {
+  int64_t row, unit;
+  item_of(units, row, unit);
+  if (row >= c.T) return;
+  const int64_t at = unit * N, left = c.d - at, t = token_at(c, row);
+  const bool pad = c.padding >= 0 && t == c.padding, bad = !pad && (t < 0 || t >= c.V);
+  float v[N];
+  load_n<N>(E + (pad || bad ? 0 : t) * ld + at, left, v);
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = bad ? __builtin_nanf("") : pad ? 0.f : v[e] * c.scale;
+  store_any<N>(out, out_type, row * ld_out + at, left, v);
+}
+
+// One unit of one chunk of positions (see the top).  A bag belongs to the chunk that holds its start; an
+// empty one at the very end to the last chunk.
+template <int N, class TE>
+__global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
+                                                   int32_t out_type, int64_t ld_out, int64_t units, int64_t L,
+                                                   int64_t chunks, float *__restrict__ part, int32_t *__restrict__ pcount) {
+  int64_t ch, unit;
+  item_of(units, ch, unit);
+  if (ch >= chunks) return;
+  const int64_t at = unit * N, left = c.d - at, dp = units * N;
+  const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
+  int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i0);
+  bool head = b > c.B || c.bags[b] != i0;
+  if (head) --b;
+  for (; b >= 0 && b < c.B; ++b, head = false) {
+    const int64_t s0 = c.bags[b], s1 = c.bags[b + 1];
+    if (!head && s0 >= i1 && i1 < c.T) break;
+    const int64_t lo = max(s0, i0), hi = min(s1, i1);
+    float acc[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    int used = 0;
+    sum_tokens<N>(c, E, ld, lo, hi, at, left, acc, used);
+    const bool more = s1 > i1 && i1 < c.T;
+    if (head || more) {
+      const int64_t p = ch * 2 + (head ? 0 : 1);
+      store_n<N>(part + p * dp + at, N, acc);
+      if (unit == 0) pcount[p] = used;
+    } else {
+      const float w = bag_weight(c, used);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] *= w;
+      store_any<N>(out, out_type, b * ld_out + at, left, acc);
+    }
+    if (more) break;
+  }
+}
+
+constexpr int JU = 16, JS = EB / JU;  // a join: units side by side, slices of the chunks
+
+// acc = the tail of chunk ch and the heads of chunks ch + 1 .. last, in slices joined in order; valid in the
+// threads of slice 0.
+template <int N>
+__device__ __forceinline__ void join_parts(const float *__restrict__ part, int64_t dp, int64_t at, bool in, int64_t ch,
+                                           int64_t last, float (&acc)[N], float (*lds)[JU][N]) {
+  const int u = threadIdx.x % JU, sl = threadIdx.x / JU;
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  if (in) {
+    const int64_t count = last - ch + 1, per = (count + JS - 1) / JS;
+    const int64_t k1 = min(count, (sl + 1) * per);
+#pragma unroll 4
+    for (int64_t k = sl * per; k < k1; ++k) {
+      float v[N];
+      load_n<N>(part + ((ch + k) * 2 + (k == 0 ? 1 : 0)) * dp + at, N, v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += v[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) lds[sl][u][e] = acc[e];
+  __syncthreads();
+  if (sl == 0)
+    for (int k = 1; k < JS; ++k)
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += lds[k][u][e];
+}
+
+// Workgroup (x, y): the bag that starts in chunk x and goes on past its end, if there is one; units 16 y ..
+template <int N>
+__global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32_t out_type, int64_t ld_out, int64_t units,
+                                                   int64_t L, const float *__restrict__ part,
+                                                   const int32_t *__restrict__ pcount) {
+  __shared__ float lds[JS][JU][N];
+  __shared__ int counts[EB / 64];
+  const int64_t ch = blockIdx.x, i0 = ch * L, i1 = min(c.T, i0 + L);
+  if (i1 >= c.T) return;
+  const int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i1) - 1;
+  if (b < 0 || b >= c.B || c.bags[b] < i0 || c.bags[b + 1] <= i1) return;
+  const int64_t last = (min(c.bags[b + 1], c.T) - 1) / L;
+  const int64_t unit = (int64_t)blockIdx.y * JU + threadIdx.x % JU, at = unit * N;
+  int used = 0;
+  for (int64_t k = threadIdx.x; k <= last - ch; k += EB) used += pcount[(ch + k) * 2 + (k == 0 ? 1 : 0)];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) used += __shfl_xor(used, o);
+  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = used;
+  float acc[N];
+  join_parts<N>(part, units * N, at, unit < units, ch, last, acc, lds);
+  if (threadIdx.x >= JU || unit >= units) return;
+  const float w = bag_weight(c, counts[0] + counts[1] + counts[2] + counts[3]);
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] *= w;
+  store_any<N>(out, out_type, b * ld_out + at, c.d - at, acc);
+}
+
+// ---------------------------------------------------------------------------- gradient
+
+struct GradSpace {
+  uint32_t *key[2], *src[2];  // [T]: token (V: none) and bag, before and after a pass of the sort
+  uint32_t *hist;             // [SORT_BLOCKS][256]
+  int32_t *count;             // [B]: positions of a bag that count (mean)
+  float *part;                // [chunks][2][d padded]
+};
+
+GradSpace grad_views(void *ws, int64_t T, int64_t B) {
+  char *p = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+  const auto take = [&](int64_t bytes) {
+    char *q = p;
+    p += div_up(bytes, 256) * 256;
+    return q;
+  };
+  GradSpace g;
+  for (int k = 0; k < 2; ++k) {
+    g.key[k] = reinterpret_cast<uint32_t *>(take(4 * T));
+    g.src[k] = reinterpret_cast<uint32_t *>(take(4 * T));
+  }
+  g.hist = reinterpret_cast<uint32_t *>(take(4LL * SORT_BLOCKS * 256));
+  g.count = reinterpret_cast<int32_t *>(take(4 * B));
+  g.part = reinterpret_cast<float *>(p);
+  return g;
+}
+
+__device__ __forceinline__ uint32_t key_at(const EmbedCall &c, int64_t i) {
+  const int64_t t = token_at(c, i);
+  return t < 0 || t >= c.V || (c.padding >= 0 && t == c.padding) ? (uint32_t)c.V : (uint32_t)t;
+}
+
+__global__ void __launch_bounds__(EB) zero_counts_k(int32_t *__restrict__ count, int64_t B) {
+  const int64_t i = (int64_t)blockIdx.x * EB + threadIdx.x;
+  if (i < B) count[i] = 0;
+}
+
+// Positions of bag b that count, from its position i.  Without padding the first position writes the
+// length; with it the positions add themselves up (whole numbers, so their order does not matter).  Out of
+// range tokens count, as they do in the sums that they make NaN.
+__device__ __forceinline__ void count_position(const EmbedCall &c, int64_t i, int64_t b, int32_t *__restrict__ count) {
+  if (c.padding < 0) {
+    if (i == c.bags[b]) count[b] = (int32_t)(c.bags[b + 1] - i);
+    return;
+  }
+  const bool live = token_at(c, i) != c.padding;
+  // the lanes of a wave that share the first lane's bag (all of them in a long bag) add up in one go
+  const int64_t first = ((int64_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
+  const unsigned long long same = __ballot(b == first && live);
+  if (b == first) {
+    if (live && (threadIdx.x & 63) == __builtin_ctzll(same)) atomicAdd(&count[b], __popcll(same));
+  } else if (live) {
+    atomicAdd(&count[b], 1);
+  }
+}
+
+// Zeros to this block's share of dE (blk of `blocks`), rows of `d` values ld apart.
+__device__ __forceinline__ void zero_rows(void *de, int32_t type, int64_t rows, int64_t d, int64_t ld, int64_t blk,
+                                          int64_t blocks) {
+  if (ld == d) {
+    d *= rows;
+    ld = d;
+    rows = 1;
+  }
+  constexpr int N = 8;
+  const int64_t units = (d + N - 1) / N;
+  const float z[N] = {};
+  for (int64_t r = 0; r < rows; ++r) {
+    if (rows > 1 && r % blocks != blk) continue;
+    for (int64_t u = (rows > 1 ? 0 : blk * EB) + threadIdx.x; u < units; u += rows > 1 ? EB : blocks * EB)
+      store_any<N>(de, type, r * ld + u * N, d - u * N, z);
+  }
+}
+
+struct FillCall {
+  void *de;
+  int32_t type;
+  int64_t rows, d, ld, blocks;
+};
+
+// Up to RANK_MAX positions: the place of a position is the number of positions with a smaller token, or the
+// same token and a smaller index.  64 positions a workgroup, a quarter of the comparisons a wave.  Blocks
+// past those zero dE meanwhile.
+__global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks) {
+  if ((int64_t)blockIdx.x >= sort_blocks) {
+    zero_rows(f.de, f.type, f.rows, f.d, f.ld, blockIdx.x - sort_blocks, f.blocks);
+    return;
+  }
+  extern __shared__ uint32_t keys[];
+  __shared__ int ranks[EB / 64][64];
+  const int T = (int)c.T, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int Tp = (T + 15) / 16 * 16;
+  for (int j = threadIdx.x; j < Tp; j += EB) keys[j] = j < T ? key_at(c, j) : 0xffffffffu;
+  __syncthreads();
+  const int p0 = blockIdx.x * 64, i = p0 + lane;
+  const uint32_t k = i < T ? keys[i] : 0u;
+  const int quarter = Tp / 4;
+  const int j0 = w * quarter, j1 = j0 + quarter;
+  int rank = 0;
+  for (int j = j0; j < j1; j += 4) {
+    const uint4 o = *reinterpret_cast<const uint4 *>(&keys[j]);
+    if (j + 4 <= p0) {
+      rank += (o.x <= k) + (o.y <= k) + (o.z <= k) + (o.w <= k);
+    } else if (j >= p0 + 64) {
+      rank += (o.x < k) + (o.y < k) + (o.z < k) + (o.w < k);
+    } else {
+      rank += (o.x < k || (o.x == k && j < i)) + (o.y < k || (o.y == k && j + 1 < i)) +
+              (o.z < k || (o.z == k && j + 2 < i)) + (o.w < k || (o.w == k && j + 3 < i));
+    }
+  }
+  ranks[w][lane] = rank;
+  __syncthreads();
+  if (w != 0 || i >= T) return;
+  rank = ranks[0][lane] + ranks[1][lane] + ranks[2][lane] + ranks[3][lane];
+  const int64_t b = bag_at(c, i);
+  g.key[0][rank] = k;
+  g.src[0][rank] = (uint32_t)b;
+  if (c.mean && c.bags) count_position(c, i, b, g.count);
+}
+
+// More positions: a stable radix sort, 8 bits a pass.  Block b holds `per` consecutive positions.  This
+// kernel makes keys and bags and counts the first digit of every block; blocks past the sort's zero dE.
+__global__ void __launch_bounds__(EB) embed_expand_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks, int64_t per) {
+  if ((int64_t)blockIdx.x >= sort_blocks) {
+    zero_rows(f.de, f.type, f.rows, f.d, f.ld, blockIdx.x - sort_blocks, f.blocks);
+    return;
+  }
+  __shared__ uint32_t h[256];
+  h[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t i1 = min(c.T, (blockIdx.x + 1) * per);
+  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += EB) {
+    const uint32_t k = key_at(c, i);
+    const int64_t b = bag_at(c, i);
+    g.key[0][i] = k;
+    g.src[0][i] = (uint32_t)b;
+    if (c.mean && c.bags) count_position(c, i, b, g.count);
+    atomicAdd(&h[k & 255], 1u);
+  }
+  __syncthreads();
+  g.hist[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(EB) radix_count_k(const uint32_t *__restrict__ key, int64_t T, int shift, int64_t per,
+                                                    uint32_t *__restrict__ hist) {
+  __shared__ uint32_t h[256];
+  h[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t i1 = min(T, (blockIdx.x + 1) * per);
+  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += EB) atomicAdd(&h[(key[i] >> shift) & 255], 1u);
+  __syncthreads();
+  hist[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
+}
+
+// Every position of this block to its place: the positions with a smaller digit, those with its digit in
+// blocks before, and those before it in this block, 256 of them at a time (a wave counts its own by
+// ballots over the digit's bits).
+__global__ void __launch_bounds__(EB) radix_place_k(const uint32_t *__restrict__ key, const uint32_t *__restrict__ src,
+                                                    uint32_t *__restrict__ key_out, uint32_t *__restrict__ src_out,
+                                                    int64_t T, int shift, int64_t per, const uint32_t *__restrict__ hist) {
+  __shared__ uint32_t base[256];          // next place of each digit
+  __shared__ uint32_t wave_n[EB / 64][256];
+  __shared__ uint32_t wsum[EB / 64];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  uint32_t before = 0, total = 0;
+#pragma unroll 16
+  for (int b = 0; b < (int)gridDim.x; ++b) {
+    const uint32_t v = hist[b * 256 + t];
+    before += b < (int)blockIdx.x ? v : 0;
+    total += v;
+  }
+  uint32_t incl = total;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = __shfl_up(incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  uint32_t b0 = incl - total + before;
+  for (int q = 0; q < w; ++q) b0 += wsum[q];
+  base[t] = b0;
+#pragma unroll
+  for (int q = 0; q < EB / 64; ++q) wave_n[q][t] = 0;
+  __syncthreads();
+  const int64_t i0 = blockIdx.x * per, i1 = min(T, i0 + per);
+  for (int64_t r = i0; r < i1; r += EB) {
+    const int64_t i = r + t;
+    const bool in = i < i1;
+    const uint32_t k = in ? key[i] : 0, dig = (k >> shift) & 255;
+    const uint32_t s = in ? src[i] : 0;
+    unsigned long long same = __ballot(in);
+#pragma unroll
+    for (int bit = 0; bit < 8; ++bit) {
+      const unsigned long long m = __ballot(in && ((dig >> bit) & 1));
+      same &= (dig >> bit) & 1 ? m : ~m;
+    }
+    const uint32_t mine = __popcll(same & ((1ull << lane) - 1ull));
+    if (in && mine == 0) wave_n[w][dig] = __popcll(same);
+    __syncthreads();
+    if (in) {
+      uint32_t at = base[dig] + mine;
+      for (int q = 0; q < w; ++q) at += wave_n[q][dig];
+      key_out[at] = k;
+      src_out[at] = s;
+    }
+    __syncthreads();
+    uint32_t add = 0;
+#pragma unroll
+    for (int q = 0; q < EB / 64; ++q) {
+      add += wave_n[q][t];
+      wave_n[q][t] = 0;
+    }
+    base[t] += add;
+    __syncthreads();
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void put_row(void *de, int32_t type, int64_t at, int64_t left, bool accumulate, float (&acc)[N]) {
+  if (accumulate) {
+    float old[N];
+    load_any<N>(de, type, at, left, old);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] += old[e];
+  }
+  store_any<N>(de, type, at, left, acc);
+}
+
+// One unit of one chunk of the sorted positions (see the top).
+template <int N, class TY>
+__global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *__restrict__ key,
+                                                   const uint32_t *__restrict__ src, const int32_t *__restrict__ count,
+                                                   const TY *__restrict__ dy, int64_t ld, void *de, int32_t de_type,
+                                                   int64_t ld_de, int32_t accumulate, int64_t units, int64_t L,
+                                                   int64_t chunks, float *__restrict__ part) {
+  int64_t ch, unit;
+  item_of(units, ch, unit);
+  if (ch >= chunks) return;
+  const int64_t at = unit * N, left = c.d - at, dp = units * N;
+  const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
+  uint32_t run = key[i0];
+  bool head = i0 > 0 && key[i0 - 1] == run;  // the run began before this chunk
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  const bool mean = c.mean && c.bags;
+  for (int64_t i = i0; i < i1 && run < (uint32_t)c.V; i += EU) {
+    float v[EU][N], wt[EU];
+    uint32_t k[EU];
+#pragma unroll
+    for (int q = 0; q < EU; ++q) {
+      const int64_t j = min(i + q, i1 - 1);
+      k[q] = key[j];
+      const int64_t b = src[j];
+      wt[q] = mean ? c.scale / (float)count[b] : c.scale;
+      load_n<N>(dy + b * ld + at, left, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < EU; ++q) {
+      if (i + q >= i1) break;
+      if (k[q] != run) {
+        if (head)
+          store_n<N>(part + ch * 2 * dp + at, N, acc);
+        else if (run < (uint32_t)c.V)
+          put_row<N>(de, de_type, run * ld_de + at, left, accumulate, acc);
+        head = false;
+        run = k[q];
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = __builtin_fmaf(wt[q], v[q][e], acc[e]);
+    }
+  }
+  if (run >= (uint32_t)c.V) return;
+  const bool more = i1 < c.T && key[i1] == run;
+  if (head || more)
+    store_n<N>(part + (ch * 2 + (head ? 0 : 1)) * dp + at, N, acc);
+  else
+    put_row<N>(de, de_type, run * ld_de + at, left, accumulate, acc);
+}
+
+// Workgroup (x, y): the token whose run starts in chunk x and goes on past its end, if there is one.
+template <int N>
+__global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint32_t *__restrict__ key, void *de,
+                                                        int32_t de_type, int64_t ld_de, int32_t accumulate,
+                                                        int64_t units, int64_t L, const float *__restrict__ part) {
+  __shared__ float lds[JS][JU][N];
+  const int64_t ch = blockIdx.x, i0 = ch * L, i1 = min(c.T, i0 + L);
+  if (i1 >= c.T) return;
+  const uint32_t run = key[i1];
+  if (run >= (uint32_t)c.V || key[i1 - 1] != run || (i0 > 0 && key[i0 - 1] == run)) return;
+  const int64_t end = i1 + lower_bound<uint32_t>(key + i1, c.T - i1, run + 1);
+  const int64_t unit = (int64_t)blockIdx.y * JU + threadIdx.x % JU, at = unit * N;
+  float acc[N];
+  join_parts<N>(part, units * N, at, unit < units, ch, (end - 1) / L, acc, lds);
+  if (threadIdx.x >= JU || unit >= units) return;
+  put_row<N>(de, de_type, run * ld_de + at, c.d - at, accumulate, acc);
+}
+
+__global__ void __launch_bounds__(EB) embed_check_k(EmbedCall c, int32_t *__restrict__ invalid) {
+  const int64_t step = (int64_t)gridDim.x * EB, i0 = (int64_t)blockIdx.x * EB + threadIdx.x;
+  bool bad = false;
+  for (int64_t i = i0; i < c.T; i += step) {
+    const int64_t t = token_at(c, i);
+    bad = bad || ((t < 0 || t >= c.V) && !(c.padding >= 0 && t == c.padding));
+  }
+  if (c.bags) {
+    for (int64_t b = i0; b <= c.B; b += step) {
+      const int64_t s = c.bags[b];
+      bad = bad || s < 0 || s > c.T || (b == 0 && s != 0) || (b == c.B ? s != c.T : s > c.bags[b + 1]);
+    }
+  }
+  if (bad) *invalid = 1;
+}
+
+template <class F>
+hipError_t by_type(int32_t type, F f) {
+  if (type == SVM_F32) return f((const float *)nullptr);
+  if (type == SVM_BF16) return f((const __bf16 *)nullptr);
+  return f((const _Float16 *)nullptr);
+}
+
+bool grid_fits(int64_t blocks) { return blocks <= 0x7fffffffLL; }
+
+int64_t part_floats(int64_t T, int64_t d) { return div_up(T > 0 ? T : 1, chunk_of(T, d)) * 2 * div_up(d, 8) * 8; }
+
+}  // namespace
+
+int64_t embed_scratch_bytes(int64_t T, int64_t d, int64_t, bool bags) {
+  if (!bags) return 0;
+  return 4 * part_floats(T, d) + 8 * div_up(T > 0 ? T : 1, chunk_of(T, d)) + 512;
+}
+
+hipError_t launch_embed_check(const EmbedCall &c, int32_t *invalid, hipStream_t s) {
+  const int64_t work = c.T > c.B + 1 ? c.T : c.B + 1;
+  const int64_t blocks = div_up(work, EB) > 2048 ? 2048 : div_up(work, EB);
+  hipLaunchKernelGGL(embed_check_k, dim3((unsigned)blocks), dim3(EB), 0, s, c, invalid);
+  return hipGetLastError();
+}
+
+hipError_t launch_embed(const EmbedCall &c, const void *table, int32_t table_type, int64_t ld_table, void *out,
+                        int32_t out_type, int64_t ld_out, void *ws, hipStream_t s) {
+  if (c.B <= 0) return hipSuccess;
+  return by_type(table_type, [&](auto *tag) -> hipError_t {
+    using TE = std::remove_cv_t<std::remove_pointer_t<decltype(tag)>>;
+    constexpr int N = UNIT<TE>;
+    const TE *E = static_cast<const TE *>(table);
+    const int64_t units = div_up(c.d, N);
+    if (!c.bags) {
+      const int64_t blocks = div_up(c.T * units, EB);
+      if (!grid_fits(blocks)) return hipErrorInvalidValue;
+      hipLaunchKernelGGL((embed_rows_k<N, TE>), dim3((unsigned)blocks), dim3(EB), 0, s, c, E, ld_table, out, out_type,
+                         ld_out, units);
+      return hipGetLastError();
+    }
+    const int64_t L = chunk_of(c.T, c.d), chunks = c.T > 0 ? div_up(c.T, L) : 1;
+    const int64_t blocks = div_up(chunks * units, EB);
+    if (!grid_fits(blocks) || div_up(units, JU) > 65535) return hipErrorInvalidValue;
+    float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+    int32_t *pcount = reinterpret_cast<int32_t *>(part + chunks * 2 * units * N);
+    hipLaunchKernelGGL((embed_bags_k<N, TE>), dim3((unsigned)blocks), dim3(EB), 0, s, c, E, ld_table, out, out_type, ld_out,
+                       units, L, chunks, part, pcount);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || chunks == 1) return e;
+    hipLaunchKernelGGL((embed_join_k<N>), dim3((unsigned)chunks, (unsigned)div_up(units, JU)), dim3(EB), 0, s, c, out,
+                       out_type, ld_out, units, L, part, pcount);
+    return hipGetLastError();
+  });
+}
+
+int64_t embed_grad_scratch_bytes(int64_t T, int64_t d, int64_t B) {
+  return 16 * T + 4LL * SORT_BLOCKS * 256 + 4 * B + 4 * part_floats(T, d) + 8 * 256;
+}
+
+hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type, int64_t ld_dy, void *de,
+                             int32_t de_type, int64_t ld_de, bool accumulate, void *ws, hipStream_t s) {
+  const GradSpace g = grad_views(ws, c.T, c.B);
+  FillCall f{de, de_type, c.V, c.d, ld_de, 0};
+  if (!accumulate) {
+    const int64_t units = ld_de == c.d ? div_up(c.V * c.d, 8 * EB) : c.V;
+    f.blocks = units > 2048 ? 2048 : units;
+  }
+  const bool counted = c.mean && c.bags && c.padding >= 0 && c.T > 0;
+  if (counted) hipLaunchKernelGGL(zero_counts_k, dim3((unsigned)div_up(c.B, EB)), dim3(EB), 0, s, g.count, c.B);
+  int cur = 0;
+  if (c.T <= RANK_MAX) {
+    const int64_t blocks = div_up(c.T, 64);
+    if (blocks + f.blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL(embed_rank_k, dim3((unsigned)(blocks + f.blocks)), dim3(EB), (size_t)div_up(c.T, 16) * 64, s, c, g, f,
+                       blocks);
+  } else {
+    const int64_t want = div_up(c.T, 2048), nb0 = want > SORT_BLOCKS ? SORT_BLOCKS : want;
+    const int64_t per = div_up(div_up(c.T, nb0), EB) * EB, nb = div_up(c.T, per);
+    hipLaunchKernelGGL(embed_expand_k, dim3((unsigned)(nb + f.blocks)), dim3(EB), 0, s, c, g, f, nb, per);
+    int bits = 0;
+    while (bits < 32 && (c.V >> bits) > 0) bits += 8;  // the keys are 0 .. V
+    for (int shift = 0; shift < bits; shift += 8) {
+      if (shift > 0)
+        hipLaunchKernelGGL(radix_count_k, dim3((unsigned)nb), dim3(EB), 0, s, g.key[cur], c.T, shift, per, g.hist);
+      hipLaunchKernelGGL(radix_place_k, dim3((unsigned)nb), dim3(EB), 0, s, g.key[cur], g.src[cur], g.key[1 - cur],
+                         g.src[1 - cur], c.T, shift, per, g.hist);
+      cur = 1 - cur;
+    }
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || c.T == 0) return e;
+  return by_type(dy_type, [&](auto *tag) -> hipError_t {
+    using TY = std::remove_cv_t<std::remove_pointer_t<decltype(tag)>>;
+    constexpr int N = UNIT<TY>;
+    const int64_t units = div_up(c.d, N), L = chunk_of(c.T, c.d), chunks = div_up(c.T, L);
+    const int64_t blocks = div_up(chunks * units, EB);
+    if (!grid_fits(blocks) || div_up(units, JU) > 65535) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((embed_runs_k<N, TY>), dim3((unsigned)blocks), dim3(EB), 0, s, c, g.key[cur], g.src[cur], g.count,
+                       static_cast<const TY *>(dy), ld_dy, de, de_type, ld_de, accumulate ? 1 : 0, units, L, chunks, g.part);
+    hipError_t e2 = hipGetLastError();
+    if (e2 != hipSuccess || chunks == 1) return e2;
+    hipLaunchKernelGGL((embed_runs_join_k<N>), dim3((unsigned)chunks, (unsigned)div_up(units, JU)), dim3(EB), 0, s, c,
+                       g.key[cur], de, de_type, ld_de, accumulate ? 1 : 0, units, L, g.part);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace svmx

@@ -1,0 +1,243 @@
+// layers.cpp -- the C ABI of the operators around a machine whose rows are learned from tokens (declared in
+// include/svmx.h): argument checks, then one launcher each.  Nothing here waits for the device.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "common.hpp"
+#include "layers.hpp"
+#include "status.hpp"
+
+using namespace svmx;
+
+namespace {
+
+constexpr int64_t INDEX_MAX = 0x7ffffffeLL;  // sizes that the kernels index in 32 bits
+
+bool float_type(int32_t t) { return t == SVM_F32 || t == SVM_BF16 || t == SVM_F16; }
+
+// Whether rows x ld values, and bytes of them, fit 64 bits.
+bool fits(int64_t rows, int64_t ld) { return ld <= (INT64_MAX / 64) / (rows > 0 ? rows : 1); }
+
+svm_status check_workspace(const void *ws, int64_t have, int64_t need) {
+  if (need > 0 && (!ws || have < need))
+    return fail(SVM_EWORKSPACE, "workspace of %lld bytes needed, %lld given", (long long)need, (long long)have);
+  return SVM_OK;
+}
+
+// What both directions of the embedding ask of their tokens and bags; fills *c.
+svm_status embed_call(const void *tokens, int32_t token_bytes, int64_t T, const int64_t *bags, int64_t B, double scale,
+                      int32_t mean, int64_t padding, int64_t V, int64_t d, EmbedCall *c) {
+  if (T < 0 || B < 0 || V < 1 || d < 1) return fail(SVM_EINVAL, "need T, B >= 0 and V, d >= 1");
+  if (T > INDEX_MAX || B > INDEX_MAX || V > INDEX_MAX || d > INDEX_MAX)
+    return fail(SVM_EINVAL, "T, B, V or d above %lld", (long long)INDEX_MAX);
+  if (token_bytes != 4 && token_bytes != 8) return fail(SVM_EINVAL, "tokens of %d bytes (4 or 8)", token_bytes);
+  if (!tokens && T > 0) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (!bags && B != T) return fail(SVM_EINVAL, "without bags there is one row a token (T=%lld, B=%lld)", (long long)T, (long long)B);
+  if (bags && B == 0 && T > 0) return fail(SVM_EINVAL, "%lld tokens in no bag", (long long)T);
+  if (!std::isfinite(scale)) return fail(SVM_EINVAL, "scale must be finite");
+  if (!fits(T + 256, d + 8)) return fail(SVM_EINVAL, "sizes overflow 64-bit byte counts");
+  c->tokens = tokens;
+  c->wide = token_bytes == 8;
+  c->mean = mean != 0;
+  c->T = T;
+  c->bags = bags;
+  c->B = B;
+  c->padding = padding;
+  c->V = V;
+  c->d = d;
+  c->scale = (float)scale;
+  return SVM_OK;
+}
+
+svm_status check_rows(const char *name, int32_t type, int64_t rows, int64_t d, int64_t ld) {
+  if (!float_type(type)) return fail(SVM_EINVAL, "%s: unknown type %d", name, type);
+  if (ld < d) return fail(SVM_EINVAL, "%s: pitch %lld below d=%lld", name, (long long)ld, (long long)d);
+  if (!fits(rows, ld)) return fail(SVM_EINVAL, "%s: sizes overflow 64-bit byte counts", name);
+  return SVM_OK;
+}
+
+#define CHECK(expr)                     \
+  do {                                  \
+    const svm_status s_ = (expr);       \
+    if (s_ != SVM_OK) return s_;        \
+  } while (0)
+
+svm_status norm_call(const void *x, int32_t x_type, int64_t n, int64_t d, int64_t ld_x, const void *weight,
+                     const void *bias, int32_t weight_type, NormCall *c) {
+  if (n < 0 || d < 1 || d > INDEX_MAX) return fail(SVM_EINVAL, "need n >= 0 and 1 <= d <= %lld", (long long)INDEX_MAX);
+  CHECK(check_rows("x", x_type, n, d, ld_x));
+  if (!x && n > 0) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (weight_type != SVM_F32 && weight_type != x_type)
+    return fail(SVM_EINVAL, "weight and bias are fp32 or of x's type (got type %d)", weight_type);
+  c->n = n;
+  c->d = d;
+  c->x = x;
+  c->x_type = x_type;
+  c->ld_x = ld_x;
+  c->w = weight;
+  c->b = bias;
+  c->w_type = weight_type;
+  return SVM_OK;
+}
+
+svm_status sv_grad(const float *X, const int32_t *y, const double *alpha, int64_t n, int64_t d, double gamma,
+                   const float *Q, int64_t m, const double *up, float *dX, void *workspace, int64_t workspace_bytes,
+                   const svm_options *o) {
+  if (n < 1 || d < 1 || m < 0) return fail(SVM_EINVAL, "need n >= 1, d >= 1, m >= 0");
+  if (!X || !y || !alpha || (m > 0 && !dX)) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (!std::isfinite(gamma) || gamma <= 0.0) return fail(SVM_EINVAL, "gamma must be finite and > 0");
+  if (n > INDEX_MAX) return fail(SVM_ENOMEM, "n=%lld exceeds the 32-bit sample index", (long long)n);
+  const int64_t need = Q ? svm_predict_grad_workspace_bytes(n, d, m) : svm_objective_grad_workspace_bytes(n, d);
+  if (need < 0) return fail(SVM_EINVAL, "sizes overflow 64-bit byte counts");
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  if (m == 0) return SVM_OK;
+  CHECK(check_workspace(workspace, workspace_bytes, need));
+  SvGradCall c{X, y, alpha, n, d, gamma, Q, up, m, dX};
+  HIPCHK(launch_sv_grad(c, workspace, s));
+  return SVM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t svm_embed_workspace_bytes(int64_t T, int64_t d, int64_t B, int32_t has_bags) {
+  if (T < 0 || B < 0 || d < 1 || T > INDEX_MAX || B > INDEX_MAX || d > INDEX_MAX || !fits(T + 256, d + 8)) return -1;
+  return embed_scratch_bytes(T, d, B, has_bags != 0);
+}
+
+svm_status svm_embed(const void *table, int32_t table_type, int64_t V, int64_t d, int64_t ld_table, const void *tokens,
+                     int32_t token_bytes, int64_t T, const int64_t *bags, int64_t B, double scale, int32_t mean,
+                     int64_t padding, void *out, int32_t out_type, int64_t ld_out, int32_t *invalid, void *workspace,
+                     int64_t workspace_bytes, const svm_options *o) {
+  clear_error();
+  EmbedCall c;
+  CHECK(embed_call(tokens, token_bytes, T, bags, B, scale, mean, padding, V, d, &c));
+  CHECK(check_rows("table", table_type, V, d, ld_table));
+  CHECK(check_rows("out", out_type, B, d, ld_out));
+  if (!table || (B > 0 && !out)) return fail(SVM_EINVAL, "NULL pointer argument");
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  if (B == 0) return SVM_OK;
+  CHECK(check_workspace(workspace, workspace_bytes, embed_scratch_bytes(T, d, B, bags != nullptr)));
+  if (invalid) HIPCHK(launch_embed_check(c, invalid, s));
+  HIPCHK(launch_embed(c, table, table_type, ld_table, out, out_type, ld_out, workspace, s));
+  return SVM_OK;
+}
+
+int64_t svm_embed_grad_workspace_bytes(int64_t T, int64_t d, int64_t B) {
+  if (T < 0 || B < 0 || d < 1 || T > INDEX_MAX || B > INDEX_MAX || d > INDEX_MAX || !fits(T + 256, d + 8)) return -1;
+  return embed_grad_scratch_bytes(T, d, B);
+}
+
+svm_status svm_embed_grad(const void *tokens, int32_t token_bytes, int64_t T, const int64_t *bags, int64_t B,
+                          double scale, int32_t mean, int64_t padding, const void *dY, int32_t dy_type, int64_t ld_dy,
+                          void *dE, int32_t de_type, int64_t V, int64_t d, int64_t ld_de, int32_t accumulate,
+                          int32_t *invalid, void *workspace, int64_t workspace_bytes, const svm_options *o) {
+  clear_error();
+  EmbedCall c;
+  CHECK(embed_call(tokens, token_bytes, T, bags, B, scale, mean, padding, V, d, &c));
+  CHECK(check_rows("dY", dy_type, B, d, ld_dy));
+  CHECK(check_rows("dE", de_type, V, d, ld_de));
+  if (!dE || (T > 0 && !dY)) return fail(SVM_EINVAL, "NULL pointer argument");
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  CHECK(check_workspace(workspace, workspace_bytes, embed_grad_scratch_bytes(T, d, B)));
+  if (invalid) HIPCHK(launch_embed_check(c, invalid, s));
+  HIPCHK(launch_embed_grad(c, dY, dy_type, ld_dy, dE, de_type, ld_de, accumulate != 0, workspace, s));
+  return SVM_OK;
+}
+
+svm_status svm_layernorm(const void *x, int32_t x_type, int64_t n, int64_t d, int64_t ld_x, const void *weight,
+                         const void *bias, int32_t weight_type, double eps, void *y, int32_t y_type, int64_t ld_y,
+                         float *mean, float *rstd, const svm_options *o) {
+  clear_error();
+  NormCall c;
+  CHECK(norm_call(x, x_type, n, d, ld_x, weight, bias, weight_type, &c));
+  CHECK(check_rows("y", y_type, n, d, ld_y));
+  if (y_type != SVM_F32 && y_type != x_type) return fail(SVM_EINVAL, "y is fp32 or of x's type (got type %d)", y_type);
+  if (!y && n > 0) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (!std::isfinite(eps) || !((float)eps > 0.f)) return fail(SVM_EINVAL, "eps must be finite and > 0 in fp32");
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  HIPCHK(launch_layernorm(c, (float)eps, y, y_type, ld_y, mean, rstd, s));
+  return SVM_OK;
+}
+
+int64_t svm_layernorm_grad_workspace_bytes(int64_t n, int64_t d, int32_t x_type) {
+  if (n < 0 || d < 1 || d > INDEX_MAX || !float_type(x_type) || !fits(n, d)) return -1;
+  return layernorm_grad_scratch_bytes(n, d, x_type);
+}
+
+svm_status svm_layernorm_grad(const void *dy, int32_t dy_type, int64_t ld_dy, const void *x, int32_t x_type, int64_t n,
+                              int64_t d, int64_t ld_x, const float *mean, const float *rstd, const void *weight,
+                              int32_t weight_type, void *dx, int64_t ld_dx, void *dweight, void *dbias, void *workspace,
+                              int64_t workspace_bytes, const svm_options *o) {
+  clear_error();
+  NormCall c;
+  CHECK(norm_call(x, x_type, n, d, ld_x, weight, nullptr, weight_type, &c));
+  CHECK(check_rows("dy", dy_type, n, d, ld_dy));
+  CHECK(check_rows("dx", x_type, n, d, ld_dx));
+  if (dy_type != SVM_F32 && dy_type != x_type) return fail(SVM_EINVAL, "dy is fp32 or of x's type (got type %d)", dy_type);
+  if (n > 0 && (!dy || !mean || !rstd || !dx)) return fail(SVM_EINVAL, "NULL pointer argument");
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  CHECK(check_workspace(workspace, workspace_bytes, layernorm_grad_scratch_bytes(n, d, x_type)));
+  HIPCHK(launch_layernorm_grad(c, dy, dy_type, ld_dy, mean, rstd, dx, ld_dx, dweight, dbias, workspace, s));
+  return SVM_OK;
+}
+
+svm_status svm_adamw(const svm_adamw_tensor *tensors, int64_t count, const svm_adamw_params *p, const svm_options *o) {
+  clear_error();
+  if (!p || count < 0 || (count > 0 && !tensors)) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (p->struct_size != (int32_t)sizeof(svm_adamw_params) || p->reserved != 0) return fail(SVM_EINVAL, "bad parameters");
+  const auto natural = [](double v) { return std::isfinite(v) && v >= 0.0; };
+  if (p->step < 1) return fail(SVM_EINVAL, "step must be >= 1 (got %lld)", (long long)p->step);
+  if (!natural(p->lr) || !natural(p->eps) || !natural(p->grad_scale))
+    return fail(SVM_EINVAL, "lr, eps and grad_scale must be finite and >= 0");
+  if (!natural(p->beta1) || !natural(p->beta2) || p->beta1 >= 1.0 || p->beta2 >= 1.0)
+    return fail(SVM_EINVAL, "beta1 and beta2 must be in [0, 1)");
+  for (int64_t i = 0; i < count; ++i) {
+    const svm_adamw_tensor &t = tensors[i];
+    if (t.count < 0 || t.count > INT64_MAX / 64 || t.reserved != 0)
+      return fail(SVM_EINVAL, "tensor %lld: bad count %lld", (long long)i, (long long)t.count);
+    if (!float_type(t.param_type) || !float_type(t.grad_type) || (t.state_type != SVM_F32 && t.state_type != SVM_F8))
+      return fail(SVM_EINVAL, "tensor %lld: unknown type", (long long)i);
+    if (!natural(t.weight_decay)) return fail(SVM_EINVAL, "tensor %lld: weight_decay must be finite and >= 0", (long long)i);
+    if (t.count > 0 && (!t.param || !t.grad || !t.m || !t.v || (t.state_type == SVM_F8 && (!t.m_scale || !t.v_scale))))
+      return fail(SVM_EINVAL, "tensor %lld: NULL pointer", (long long)i);
+  }
+  hipStream_t s;
+  if (!stream_of(o, &s)) return fail(SVM_EINVAL, "bad options");
+  HIPCHK(launch_adamw(tensors, count, *p, s));
+  return SVM_OK;
+}
+
+int64_t svm_predict_grad_workspace_bytes(int64_t n, int64_t d, int64_t m) {
+  if (n < 1 || d < 1 || m < 0 || n > INDEX_MAX || !fits(n, d + 64) || !fits(m + 256, d + 64)) return -1;
+  return sv_grad_scratch_bytes(n, d, m, false);
+}
+
+svm_status svm_predict_grad(const float *X_train, const int32_t *y, const double *alpha, int64_t n, int64_t d,
+                            double gamma, const float *X_test, int64_t m, const double *upstream, float *dX,
+                            void *workspace, int64_t workspace_bytes, const svm_options *o) {
+  clear_error();
+  if (!X_test && m > 0) return fail(SVM_EINVAL, "NULL pointer argument");
+  if (m == 0) X_test = X_train;
+  return sv_grad(X_train, y, alpha, n, d, gamma, X_test, m, upstream, dX, workspace, workspace_bytes, o);
+}
+
+int64_t svm_objective_grad_workspace_bytes(int64_t n, int64_t d) {
+  if (n < 1 || d < 1 || n > INDEX_MAX || !fits(n + 256, d + 64)) return -1;
+  return sv_grad_scratch_bytes(n, d, n, true);
+}
+
+svm_status svm_objective_grad(const float *X, const int32_t *y, const double *alpha, int64_t n, int64_t d, double gamma,
+                              float *dX, void *workspace, int64_t workspace_bytes, const svm_options *o) {
+  clear_error();
+  return sv_grad(X, y, alpha, n, d, gamma, nullptr, n, nullptr, dX, workspace, workspace_bytes, o);
+}
+
+}  // extern "C"

@@ -1,0 +1,470 @@
+// norm.hip -- layer norm of rows and its gradient.
+//
+// mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), h = (x - mu) r, y = h w + b;
+// q = dy w, dx = r (q - mean q - h mean(q h)), dw = sum over rows dy h, db = sum over rows dy.
+// Both directions are bound by memory, so a row is read once and stays in registers: a row takes G lanes of
+// a wave (a power of two, up to 64) or a whole workgroup, each lane K units of 16 bytes.  The variance is a
+// second sum over the registers, of (x - mu)^2, which loses nothing where |mu| is large.  All sums are
+// fp32; outputs are rounded once.
+// The weight's and bias's gradients: a workgroup walks rows and keeps dy h and dy of its columns in
+// registers, leaves one partial row, and a second kernel adds those in their order (no atomics, so results
+// repeat bit for bit; a launch of one workgroup writes them itself).
+// Rows longer than a workgroup holds are read again from the caches for every sum.
+#include "layers.hpp"
+#include "units.hpp"
+
+#include <type_traits>
+
+namespace svmx {
+
+namespace {
+
+constexpr int NB = 256;  // threads of a workgroup
+constexpr int NW = NB / 64;
+
+inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// How a row of `units` units is spread: g lanes (NB: the workgroup), k units a lane; k = 0: too long.
+struct RowShape {
+  int g, k;
+};
+
+RowShape row_shape(int64_t units) {
+  if (units <= 64) {
+    int g = 1;
+    while (g < units) g <<= 1;
+    return {g, 1};
+  }
+  if (units <= 256) return {64, units <= 128 ? 2 : 4};
+  if (units <= 4 * NB) return {NB, units <= 2 * NB ? 2 : 4};
+  return {NB, 0};
+}
+
+// Sums of a and b over the g lanes of a row (all of them get it); g = NB: over the workgroup.
+__device__ __forceinline__ void row_sums(float &a, float &b, int g, float (*lds)[2]) {
+  for (int o = (g < 64 ? g : 64) >> 1; o > 0; o >>= 1) {
+    a += __shfl_xor(a, o);
+    b += __shfl_xor(b, o);
+  }
+  if (g == NB) {
+    if ((threadIdx.x & 63) == 0) {
+      lds[threadIdx.x >> 6][0] = a;
+      lds[threadIdx.x >> 6][1] = b;
+    }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      a += lds[q][0];
+      b += lds[q][1];
+    }
+    __syncthreads();
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void load_weight(const void *w, int32_t type, int64_t at, int64_t left, float none, float (&v)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = none;
+  if (w) load_any<N>(w, type, at, left, v);
+}
+
+// Rows of g lanes, K units a lane; every workgroup walks rows.
+template <int K, class TX, class TY>
+__global__ void __launch_bounds__(NB) norm_k(NormCall c, int g, float eps, TY *__restrict__ y, int64_t ld_y,
+                                             float *__restrict__ mean, float *__restrict__ rstd) {
+  constexpr int N = UNIT<TX>;
+  __shared__ float lds[NW][2];
+  const TX *X = static_cast<const TX *>(c.x);
+  const int per = NB / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
+  float w[K][N], b[K][N];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int64_t at = (int64_t)(lane + k * g) * N;
+    load_weight<N>(c.w, c.w_type, at, c.d - at, 1.f, w[k]);
+    load_weight<N>(c.b, c.w_type, at, c.d - at, 0.f, b[k]);
+  }
+  const float fd = (float)c.d;  // (divided by, so that a row of one value has exactly that mean)
+  for (int64_t r0 = (int64_t)blockIdx.x * per; r0 < c.n; r0 += (int64_t)gridDim.x * per) {
+    const int64_t r = r0 + grp;
+    const bool in = r < c.n;
+    const TX *x = X + (in ? r : c.n - 1) * c.ld_x;
+    float v[K][N];
+    float s = 0.f, none = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t at = (int64_t)(lane + k * g) * N;
+      load_n<N>(x + at, c.d - at, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += v[k][e];
+    row_sums(s, none, g, lds);
+    const float mu = s / fd;
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t left = c.d - (int64_t)(lane + k * g) * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        v[k][e] -= mu;
+        if (e < left) q = __builtin_fmaf(v[k][e], v[k][e], q);
+      }
+    }
+    row_sums(q, none, g, lds);
+    const float rs = 1.0f / __builtin_sqrtf(q / fd + eps);
+    if (!in) continue;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t at = (int64_t)(lane + k * g) * N;
+      float o[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) o[e] = __builtin_fmaf(v[k][e] * rs, w[k][e], b[k][e]);
+      store_n<N>(y + r * ld_y + at, c.d - at, o);
+    }
+    if (lane == 0) {
+      if (mean) mean[r] = mu;
+      if (rstd) rstd[r] = rs;
+    }
+  }
+}
+
+// Rows longer than 4 NB units: a workgroup a row, three passes.
+template <class TX, class TY>
+__global__ void __launch_bounds__(NB) norm_long_k(NormCall c, float eps, TY *__restrict__ y, int64_t ld_y,
+                                                  float *__restrict__ mean, float *__restrict__ rstd) {
+  constexpr int N = UNIT<TX>;
+  __shared__ float lds[NW][2];
+  const int64_t units = (c.d + N - 1) / N;
+  const float fd = (float)c.d;
+  for (int64_t r = blockIdx.x; r < c.n; r += gridDim.x) {
+    const TX *x = static_cast<const TX *>(c.x) + r * c.ld_x;
+    float s = 0.f, q = 0.f, none = 0.f;
+    for (int64_t u = threadIdx.x; u < units; u += NB) {
+      float v[N];
+      load_n<N>(x + u * N, c.d - u * N, v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += v[e];
+    }
+    row_sums(s, none, NB, lds);
+    const float mu = s / fd;
+    for (int64_t u = threadIdx.x; u < units; u += NB) {
+      float v[N];
+      load_n<N>(x + u * N, c.d - u * N, v);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < c.d - u * N) q = __builtin_fmaf(v[e] - mu, v[e] - mu, q);
+    }
+    row_sums(q, none, NB, lds);
+    const float rs = 1.0f / __builtin_sqrtf(q / fd + eps);
+    for (int64_t u = threadIdx.x; u < units; u += NB) {
+      float v[N], w[N], b[N];
+      load_n<N>(x + u * N, c.d - u * N, v);
+      load_weight<N>(c.w, c.w_type, u * N, c.d - u * N, 1.f, w);
+      load_weight<N>(c.b, c.w_type, u * N, c.d - u * N, 0.f, b);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = __builtin_fmaf((v[e] - mu) * rs, w[e], b[e]);
+      store_n<N>(y + r * ld_y + u * N, c.d - u * N, v);
+    }
+    if (threadIdx.x == 0) {
+      if (mean) mean[r] = mu;
+      if (rstd) rstd[r] = rs;
+    }
+  }
+}
+
+struct NormGrad {
+  const void *dy;
+  int64_t ld_dy;
+  const float *mean, *rstd;
+  void *dx;
+  int64_t ld_dx;
+  void *dw, *db;  // NULL: not wanted
+  float *part;    // [workgroups][2][dp]
+  int64_t dp;     // units x N
+};
+
+// One column sum of the workgroup's partial rows lds[rows][dp] to part, or, where there is one workgroup, to
+// the output.
+template <int N>
+__device__ __forceinline__ void leave_sum(const NormCall &c, const float *lds, int rows, int64_t dp, float *part, void *out) {
+  for (int64_t u = threadIdx.x; u * N < dp; u += NB) {
+    float s[N] = {};
+    for (int q = 0; q < rows; ++q)
+#pragma unroll
+      for (int e = 0; e < N; ++e) s[e] += lds[q * dp + u * N + e];
+    if (gridDim.x > 1)
+      store_n<N>(part + u * N, N, s);
+    else if (out)
+      store_any<N>(out, c.w_type, u * N, c.d - u * N, s);
+  }
+}
+
+// The gradient, rows as in norm_k.  TY: type of dy (dx has x's).
+template <int K, class TX, class TY>
+__global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g) {
+  constexpr int N = UNIT<TX>;
+  extern __shared__ float cols[];  // [rows side by side][dp], in one go for dw and one for db
+  __shared__ float lds[NW][2];
+  const TX *X = static_cast<const TX *>(c.x);
+  const TY *DY = static_cast<const TY *>(p.dy);
+  TX *DX = static_cast<TX *>(p.dx);
+  const int per = NB / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
+  float w[K][N], dw[K][N], db[K][N];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int64_t at = (int64_t)(lane + k * g) * N;
+    load_weight<N>(c.w, c.w_type, at, c.d - at, 1.f, w[k]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) dw[k][e] = db[k][e] = 0.f;
+  }
+  const float fd = (float)c.d;
+  for (int64_t r0 = (int64_t)blockIdx.x * per; r0 < c.n; r0 += (int64_t)gridDim.x * per) {
+    const int64_t r = r0 + grp;
+    const bool in = r < c.n;
+    const int64_t rr = in ? r : c.n - 1;
+    float h[K][N], t[K][N];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t at = (int64_t)(lane + k * g) * N;
+      load_n<N>(X + rr * c.ld_x + at, c.d - at, h[k]);
+      load_n<N>(DY + rr * p.ld_dy + at, c.d - at, t[k]);
+    }
+    const float mu = p.mean[rr], rs = p.rstd[rr];
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        h[k][e] = (h[k][e] - mu) * rs;  // (past the row's end dy is 0)
+        const float q = t[k][e] * w[k][e];
+        s1 += q;
+        s2 = __builtin_fmaf(q, h[k][e], s2);
+        if (in) {
+          dw[k][e] = __builtin_fmaf(t[k][e], h[k][e], dw[k][e]);
+          db[k][e] += t[k][e];
+        }
+        t[k][e] = q;
+      }
+    row_sums(s1, s2, g, lds);
+    s1 /= fd;
+    s2 /= fd;
+    if (!in) continue;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t at = (int64_t)(lane + k * g) * N;
+#pragma unroll
+      for (int e = 0; e < N; ++e) t[k][e] = rs * (t[k][e] - __builtin_fmaf(h[k][e], s2, s1));
+      store_n<N>(DX + r * p.ld_dx + at, c.d - at, t[k]);
+    }
+  }
+  if (!p.dw && !p.db) return;
+  float *part = p.part + (int64_t)blockIdx.x * 2 * p.dp;
+  for (int pass = 0; pass < 2; ++pass) {
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t at = (int64_t)(lane + k * g) * N;
+      if (at < p.dp)
+#pragma unroll
+        for (int e = 0; e < N; ++e) cols[grp * p.dp + at + e] = pass == 0 ? dw[k][e] : db[k][e];
+    }
+    __syncthreads();
+    leave_sum<N>(c, cols, per, p.dp, part + pass * p.dp, pass == 0 ? p.dw : p.db);
+  }
+}
+
+// Long rows: dx a workgroup a row (two passes), and the columns' sums of a slice of rows in another kernel.
+template <class TX, class TY>
+__global__ void __launch_bounds__(NB) norm_grad_long_k(NormCall c, NormGrad p) {
+  constexpr int N = UNIT<TX>;
+  __shared__ float lds[NW][2];
+  const int64_t units = (c.d + N - 1) / N;
+  const float fd = (float)c.d;
+  for (int64_t r = blockIdx.x; r < c.n; r += gridDim.x) {
+    const TX *x = static_cast<const TX *>(c.x) + r * c.ld_x;
+    const TY *dy = static_cast<const TY *>(p.dy) + r * p.ld_dy;
+    const float mu = p.mean[r], rs = p.rstd[r];
+    float s1 = 0.f, s2 = 0.f;
+    for (int pass = 0; pass < 2; ++pass) {
+      for (int64_t u = threadIdx.x; u < units; u += NB) {
+        const int64_t left = c.d - u * N;
+        float h[N], t[N], w[N];
+        load_n<N>(x + u * N, left, h);
+        load_n<N>(dy + u * N, left, t);
+        load_weight<N>(c.w, c.w_type, u * N, left, 1.f, w);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          h[e] = (h[e] - mu) * rs;
+          t[e] *= w[e];
+          if (pass == 0) {
+            s1 += t[e];
+            s2 = __builtin_fmaf(t[e], h[e], s2);
+          } else {
+            t[e] = rs * (t[e] - __builtin_fmaf(h[e], s2, s1));
+          }
+        }
+        if (pass == 1) store_n<N>(static_cast<TX *>(p.dx) + r * p.ld_dx + u * N, left, t);
+      }
+      if (pass == 0) {
+        row_sums(s1, s2, NB, lds);
+        s1 /= fd;
+        s2 /= fd;
+      }
+    }
+  }
+}
+
+template <class TX, class TY>
+__global__ void __launch_bounds__(NB) norm_grad_cols_k(NormCall c, NormGrad p) {
+  constexpr int N = UNIT<TX>;
+  const int64_t units = (c.d + N - 1) / N, u = (int64_t)blockIdx.y * NB + threadIdx.x;
+  if (u >= units) return;
+  const int64_t per = (c.n + gridDim.x - 1) / gridDim.x, left = c.d - u * N;
+  const int64_t r1 = min(c.n, (blockIdx.x + 1) * per);
+  float dw[N] = {}, db[N] = {};
+#pragma unroll 4
+  for (int64_t r = blockIdx.x * per; r < r1; ++r) {
+    float h[N], t[N];
+    load_n<N>(static_cast<const TX *>(c.x) + r * c.ld_x + u * N, left, h);
+    load_n<N>(static_cast<const TY *>(p.dy) + r * p.ld_dy + u * N, left, t);
+    const float mu = p.mean[r], rs = p.rstd[r];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      dw[e] = __builtin_fmaf(t[e], (h[e] - mu) * rs, dw[e]);
+      db[e] += t[e];
+    }
+  }
+  float *part = p.part + (int64_t)blockIdx.x * 2 * p.dp + u * N;
+  store_n<N>(part, N, dw);
+  store_n<N>(part + p.dp, N, db);
+}
+
+constexpr int FC = 16, FS = NB / FC;  // units side by side, slices of the partial rows
+
+// dw (blockIdx.y 0) and db (1): the partial rows' sums, in slices joined in order.
+__global__ void __launch_bounds__(NB) norm_grad_sum_k(NormCall c, NormGrad p, int64_t rows) {
+  __shared__ float lds[FS][FC][4];
+  void *out = blockIdx.y == 0 ? p.dw : p.db;
+  if (!out) return;
+  const int col = threadIdx.x % FC, sl = threadIdx.x / FC;
+  const int64_t at = ((int64_t)blockIdx.x * FC + col) * 4;
+  const int64_t per = (rows + FS - 1) / FS, r1 = min(rows, (sl + 1) * per);
+  float s[4] = {};
+  if (at < p.dp) {
+#pragma unroll 8
+    for (int64_t r = sl * per; r < r1; ++r) {
+      float v[4];
+      load_n<4>(p.part + (r * 2 + blockIdx.y) * p.dp + at, 4, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) lds[sl][col][e] = s[e];
+  __syncthreads();
+  if (sl != 0 || at >= c.d) return;
+  for (int q = 1; q < FS; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += lds[q][col][e];
+  store_any<4>(out, c.w_type, at, c.d - at, s);
+}
+
+// Workgroups that walk rows: each row group takes 8 rows or more, 4 workgroups a CU at most (what their
+// partial rows cost, against what one more wave hides).
+int64_t grad_blocks(int64_t n, int g) {
+  const int64_t want = div_up(n, 8 * (NB / g));
+  return want > 1024 ? 1024 : want < 1 ? 1 : want;
+}
+int64_t cols_blocks(int64_t n) { return n > 64 * 16 ? 64 : div_up(n, 16); }
+
+int unit_of(int32_t type) { return type == SVM_F32 ? 4 : 8; }
+
+template <class TX, class F>
+hipError_t by_out(int32_t type, F f) {
+  if (type == SVM_F32) return f((TX *)nullptr, (float *)nullptr);
+  return f((TX *)nullptr, (TX *)nullptr);
+}
+
+// f(x's type, other's type): fp32, or x's type.
+template <class F>
+hipError_t by_types(int32_t x, int32_t other, F f) {
+  if (x == SVM_F32) return f((float *)nullptr, (float *)nullptr);
+  return x == SVM_BF16 ? by_out<__bf16>(other, f) : by_out<_Float16>(other, f);
+}
+
+}  // namespace
+
+hipError_t launch_layernorm(const NormCall &c, float eps, void *y, int32_t y_type, int64_t ld_y, float *mean, float *rstd,
+                            hipStream_t s) {
+  if (c.n <= 0) return hipSuccess;
+  return by_types(c.x_type, y_type, [&](auto *tx, auto *ty) -> hipError_t {
+    using TX = std::remove_pointer_t<decltype(tx)>;
+    using TY = std::remove_pointer_t<decltype(ty)>;
+    const RowShape sh = row_shape(div_up(c.d, UNIT<TX>));
+    const int64_t want = div_up(c.n, NB / sh.g), blocks = want > 4096 ? 4096 : want;
+    const auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(NB), 0, s, c, sh.g, eps, static_cast<TY *>(y), ld_y, mean, rstd);
+    };
+    if (sh.k == 1)
+      go(norm_k<1, TX, TY>);
+    else if (sh.k == 2)
+      go(norm_k<2, TX, TY>);
+    else if (sh.k == 4)
+      go(norm_k<4, TX, TY>);
+    else
+      hipLaunchKernelGGL((norm_long_k<TX, TY>), dim3((unsigned)blocks), dim3(NB), 0, s, c, eps, static_cast<TY *>(y), ld_y,
+                         mean, rstd);
+    return hipGetLastError();
+  });
+}
+
+int64_t layernorm_grad_scratch_bytes(int64_t n, int64_t d, int32_t x_type) {
+  const int64_t units = div_up(d, unit_of(x_type));
+  const RowShape sh = row_shape(units);
+  const int64_t rows = sh.k ? grad_blocks(n, sh.g) : cols_blocks(n);
+  return 8 * rows * units * unit_of(x_type) + 256;
+}
+
+hipError_t launch_layernorm_grad(const NormCall &c, const void *dy, int32_t dy_type, int64_t ld_dy, const float *mean,
+                                 const float *rstd, void *dx, int64_t ld_dx, void *dw, void *db, void *ws, hipStream_t s) {
+  if (c.n <= 0 && !dw && !db) return hipSuccess;
+  NormGrad p{dy, ld_dy, mean, rstd, dx, ld_dx, dw, db, nullptr, 0};
+  p.part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+  return by_types(c.x_type, dy_type, [&](auto *tx, auto *ty) -> hipError_t {
+    using TX = std::remove_pointer_t<decltype(tx)>;
+    using TY = std::remove_pointer_t<decltype(ty)>;
+    const int64_t units = div_up(c.d, UNIT<TX>);
+    p.dp = units * UNIT<TX>;
+    const RowShape sh = row_shape(units);
+    int64_t rows = 0;  // partial rows
+    if (c.n > 0 && sh.k) {
+      rows = grad_blocks(c.n, sh.g);
+      const size_t lds = dw || db ? (size_t)(NB / sh.g) * p.dp * 4 : 0;
+      const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(NB), lds, s, c, p, sh.g);
+      };
+      if (sh.k == 1)
+        go(norm_grad_k<1, TX, TY>);
+      else if (sh.k == 2)
+        go(norm_grad_k<2, TX, TY>);
+      else
+        go(norm_grad_k<4, TX, TY>);
+      if (rows == 1) return hipGetLastError();
+    } else if (c.n > 0) {
+      hipLaunchKernelGGL((norm_grad_long_k<TX, TY>), dim3((unsigned)(c.n > 4096 ? 4096 : c.n)), dim3(NB), 0, s, c, p);
+      if (dw || db) {
+        if (div_up(units, NB) > 65535) return hipErrorInvalidValue;
+        rows = cols_blocks(c.n);
+        hipLaunchKernelGGL((norm_grad_cols_k<TX, TY>), dim3((unsigned)rows, (unsigned)div_up(units, NB)), dim3(NB), 0, s, c, p);
+      }
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!dw && !db)) return e;
+    hipLaunchKernelGGL(norm_grad_sum_k, dim3((unsigned)div_up(p.dp, 4 * FC), 2), dim3(NB), 0, s, c, p, rows);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace svmx

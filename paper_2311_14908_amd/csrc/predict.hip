@@ -15,6 +15,7 @@
 // Few test samples (few_rule.hpp) take one pass over the training rows (predict_few) in place of all
 // of these.
 // Results are deterministic: no atomics touch values.
+#include "rbf_d2.hpp"
 #include "split_rows.hpp"
 #include "split_tile.hpp"
 
@@ -504,13 +505,6 @@ __device__ __forceinline__ few_f4u few_load(const float *__restrict__ x, int64_t
   for (int e = 0; e < 4; ++e)
     if (k + e < d) v[e] = x[k + e];
   return v;
-}
-
-// exp2(c d2), c d2 <= 0: exp2 of the fp32 part of the exponent, then the rest to first order.
-__device__ __forceinline__ double rbf_of_d2(double c, double d2) {
-  const double x2 = c * (d2 > 0.0 ? d2 : 0.0);
-  const float hi = (float)x2, e2 = __builtin_amdgcn_exp2f(hi);
-  return hi > -150.f ? (double)__builtin_fmaf(e2, 0.6931472f * (float)(x2 - (double)hi), e2) : 0.0;
 }
 
 template <int MQ>

@@ -1,0 +1,15 @@
+// rbf_d2.hpp -- the RBF kernel of a squared distance in 64 bits.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+namespace svmx {
+
+// exp2(c d2), c d2 <= 0: exp2 of the fp32 part of the exponent, then the rest to first order.
+__device__ __forceinline__ double rbf_of_d2(double c, double d2) {
+  const double x2 = c * (d2 > 0.0 ? d2 : 0.0);
+  const float hi = (float)x2, e2 = __builtin_amdgcn_exp2f(hi);
+  return hi > -150.f ? (double)__builtin_fmaf(e2, 0.6931472f * (float)(x2 - (double)hi), e2) : 0.0;
+}
+
+}  // namespace svmx

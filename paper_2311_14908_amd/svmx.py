@@ -2,14 +2,16 @@
 
 Argument marshalling only.  Device buffers are torch tensors on the current HIP device,
 workspaces are ``torch.empty(bytes, dtype=torch.uint8)`` of the size the library asks for,
-and work runs on ``torch.cuda.current_stream()``.  Every computation happens in the HIP
+and work runs on ``torch.cuda.current_stream()`` (or the call's ``stream``).  Every computation happens in the HIP
 library; if it is not built this module raises on import of the library (there is no
 fallback path).
 """
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
+import threading
 from dataclasses import dataclass
 
 import numpy as np
@@ -22,6 +24,7 @@ SVM_EINVAL, SVM_ENOMEM, SVM_EDEVICE, SVM_EWORKSPACE = -1, -2, -3, -4
 GRAM_AUTO, GRAM_ON, GRAM_OFF = 0, 1, 2
 MFMA_SPLIT_F16, MFMA_F32 = 0, 1
 SELECT_MVP, SELECT_SECOND_ORDER = 0, 1
+SVM_F32, SVM_BF16, SVM_F16, SVM_F8 = 0, 1, 2, 3
 WORKING_SET_AUTO = -1
 
 
@@ -52,6 +55,18 @@ class svm_stats(C.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class svm_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("count", C.c_int64), ("weight_decay", C.c_double),
+                ("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class svm_adamw_params(C.Structure):
+    _fields_ = [("struct_size", C.c_int32), ("reserved", C.c_int32), ("step", C.c_int64), ("lr", C.c_double),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("grad_scale", C.c_double),
+                ("grad_scale_device", C.c_void_p)]
+
+
 _STAT_NAMES = tuple(name for name, _ in svm_stats._fields_)
 _STAT_DTYPE = np.dtype(svm_stats)
 
@@ -64,7 +79,10 @@ def _stat_dicts(array):
 EXPORTS = ("svm_default_options", "svm_train_workspace_bytes", "svm_train", "svm_train_static",
            "svm_predict_workspace_bytes",
            "svm_predict", "svm_train_ovo_workspace_bytes", "svm_train_ovo", "svm_predict_ovo_workspace_bytes",
-           "svm_predict_ovo", "svm_kernel_rows", "svm_gram_workspace_bytes", "svm_gram", "svm_last_error")
+           "svm_predict_ovo", "svm_kernel_rows", "svm_gram_workspace_bytes", "svm_gram", "svm_last_error",
+           "svm_embed_workspace_bytes", "svm_embed", "svm_embed_grad_workspace_bytes", "svm_embed_grad", "svm_layernorm",
+           "svm_layernorm_grad_workspace_bytes", "svm_layernorm_grad", "svm_adamw", "svm_predict_grad_workspace_bytes",
+           "svm_predict_grad", "svm_objective_grad_workspace_bytes", "svm_objective_grad")
 
 _lib = None
 
@@ -95,6 +113,18 @@ def load(path: str | None = None):
         "svm_gram_workspace_bytes": (I64, [I64, I64, OP]),
         "svm_gram": (C.c_int, [V, I64, I64, D, V, I64, V, I64, OP]),
         "svm_last_error": (C.c_char_p, []),
+        "svm_embed_workspace_bytes": (I64, [I64, I64, I64, I32]),
+        "svm_embed": (C.c_int, [V, I32, I64, I64, I64, V, I32, I64, V, I64, D, I32, I64, V, I32, I64, V, V, I64, OP]),
+        "svm_embed_grad_workspace_bytes": (I64, [I64, I64, I64]),
+        "svm_embed_grad": (C.c_int, [V, I32, I64, V, I64, D, I32, I64, V, I32, I64, V, I32, I64, I64, I64, I32, V, V, I64, OP]),
+        "svm_layernorm": (C.c_int, [V, I32, I64, I64, I64, V, V, I32, D, V, I32, I64, V, V, OP]),
+        "svm_layernorm_grad_workspace_bytes": (I64, [I64, I64, I32]),
+        "svm_layernorm_grad": (C.c_int, [V, I32, I64, V, I32, I64, I64, I64, V, V, V, I32, V, I64, V, V, V, I64, OP]),
+        "svm_adamw": (C.c_int, [V, I64, C.POINTER(svm_adamw_params), OP]),
+        "svm_predict_grad_workspace_bytes": (I64, [I64, I64, I64]),
+        "svm_predict_grad": (C.c_int, [V, V, V, I64, I64, D, V, I64, V, V, V, I64, OP]),
+        "svm_objective_grad_workspace_bytes": (I64, [I64, I64]),
+        "svm_objective_grad": (C.c_int, [V, V, V, I64, I64, D, V, V, I64, OP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -362,3 +392,296 @@ def ovo_offsets(label: np.ndarray, k: int):
             sizes.append(int(cnt[a] + cnt[b]))
             o += int(cnt[a] + cnt[b])
     return np.array(offs), np.array(sizes)
+
+
+# ------------------------------------------------------------------ rows that are learned from tokens
+#
+# These calls queue their work on the current stream (or ``stream=``) and return without waiting.
+
+_FLOATS = {torch.float32: SVM_F32, torch.bfloat16: SVM_BF16, torch.float16: SVM_F16}
+_TOKENS = {torch.int32: 4, torch.int64: 8}
+_STATES = {torch.float32: SVM_F32, torch.float8_e4m3fn: SVM_F8}
+_tls = threading.local()
+
+
+def _stream_options():
+    """This thread's options with nothing set but the current stream."""
+    o = getattr(_tls, "options", None)
+    if o is None:
+        o = _tls.options = svm_options()
+        load().svm_default_options(C.byref(o))
+    o.stream = torch.cuda.current_stream().cuda_stream
+    return C.byref(o)
+
+
+def _tensors(args):
+    for a in args:
+        if isinstance(a, torch.Tensor):
+            yield a
+        elif isinstance(a, (list, tuple)):
+            yield from _tensors(a)
+
+
+def _streamed(f):
+    """``stream=``: run the call, and allocate what it returns, on that stream; the tensors it is given are kept
+    from being reused until the stream is done with them (waiting for them first is the caller's business)."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        for t in _tensors(list(args) + list(kw.values())):
+            if t.is_cuda:
+                t.record_stream(stream)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return call
+
+
+def _on_device(t, name):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == torch.cuda.current_device()):
+        raise TypeError(f"{name} must be a tensor on the current device")
+
+
+def _float_rows(t, name, shape=None):
+    """Type and pitch of a matrix of floats whose rows are contiguous."""
+    _on_device(t, name)
+    if t.dtype not in _FLOATS:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be a matrix" + (f" of shape {shape}" if shape else "") + f" (got {tuple(t.shape)})")
+    n, d = t.shape
+    if (d > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < d):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
+    return _FLOATS[t.dtype], t.stride(0) if n > 1 else max(d, 1)
+
+
+def _vector(t, dtype, n, name):
+    _on_device(t, name)
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} vector of {n} (got {t.dtype} {tuple(t.shape)})")
+    return t.data_ptr()
+
+
+def _workspace(nbytes, device):
+    if nbytes < 0:
+        raise SvmError(SVM_EINVAL, "workspace size query failed")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _token_args(tokens, bags, rows):
+    _on_device(tokens, "tokens")
+    if tokens.dtype not in _TOKENS or tokens.dim() != 1 or not tokens.is_contiguous():
+        raise TypeError("tokens must be a contiguous int32 or int64 vector")
+    T = tokens.shape[0]
+    if bags is None:
+        return T, T, None
+    _on_device(bags, "bags")
+    if bags.dim() != 1 or bags.shape[0] < 1 or (rows is not None and bags.shape[0] != rows + 1):
+        raise ValueError("bags must hold the start of every bag and the end of the last")
+    return T, bags.shape[0] - 1, _vector(bags, torch.int64, bags.shape[0], "bags")
+
+
+def _raise_invalid(invalid):
+    if invalid is not None and int(invalid.item()):
+        raise SvmError(SVM_EINVAL, "a token outside the table, or bags that do not run from 0 to the number of tokens")
+
+
+@_streamed
+def svm_embed(table, tokens, *, bags=None, scale: float = 1.0, mean: bool = False, padding: int = -1, out_dtype=None,
+              check: bool = True) -> torch.Tensor:
+    """Embedding bags: row b is scale * the sum (``mean``: the mean) of table[t] over the tokens t of bag b,
+    those equal to ``padding`` left out.  ``bags``: int64 starts of the bags and the end of the last, or None for
+    a row a token.  ``check`` waits for the device's word on tokens and bags and raises on invalid ones; without
+    it a token outside the table makes its row NaN."""
+    lib = load()
+    ttype, ld = _float_rows(table, "table")
+    V, d = table.shape
+    T, B, bp = _token_args(tokens, bags, None)
+    out = torch.empty((B, d), dtype=out_dtype or table.dtype, device=table.device)
+    otype, ldo = _float_rows(out, "out")
+    ws = _workspace(lib.svm_embed_workspace_bytes(T, d, B, bp is not None), table.device)
+    invalid = torch.zeros(1, dtype=torch.int32, device=table.device) if check else None
+    _check(lib.svm_embed(table.data_ptr(), ttype, V, d, ld, tokens.data_ptr(), _TOKENS[tokens.dtype], T, bp, B, scale,
+                         int(mean), padding, out.data_ptr(), otype, ldo, _ptr(invalid), _ptr(ws),
+                         0 if ws is None else ws.shape[0], _stream_options()))
+    _raise_invalid(invalid)
+    return out
+
+
+@_streamed
+def svm_embed_grad(tokens, dY, V: int, *, bags=None, scale: float = 1.0, mean: bool = False, padding: int = -1,
+                   out_dtype=None, out=None, check: bool = True) -> torch.Tensor:
+    """Gradient of svm_embed in its table of V rows, given the rows' gradients dY.  ``out``: a table's gradient to
+    add to (returned); else a new one of ``out_dtype`` (default: dY's)."""
+    lib = load()
+    T, B, bp = _token_args(tokens, bags, None)
+    ytype, ldy = _float_rows(dY, "dY", (B, dY.shape[-1]))
+    d = dY.shape[1]
+    dE = torch.empty((V, d), dtype=out_dtype or dY.dtype, device=dY.device) if out is None else out
+    etype, lde = _float_rows(dE, "out", (V, d))
+    ws = _workspace(lib.svm_embed_grad_workspace_bytes(T, d, B), dY.device)
+    invalid = torch.zeros(1, dtype=torch.int32, device=dY.device) if check else None
+    _check(lib.svm_embed_grad(tokens.data_ptr(), _TOKENS[tokens.dtype], T, bp, B, scale, int(mean), padding, dY.data_ptr(),
+                              ytype, ldy, dE.data_ptr(), etype, V, d, lde, int(out is not None), _ptr(invalid), _ptr(ws),
+                              ws.shape[0], _stream_options()))
+    _raise_invalid(invalid)
+    return dE
+
+
+def _weight_args(x, weight, bias):
+    d = x.shape[1]
+    given = weight if weight is not None else bias
+    wdtype = torch.float32 if given is None else given.dtype
+    wp = None if weight is None else _vector(weight, wdtype, d, "weight")
+    bp = None if bias is None else _vector(bias, wdtype, d, "bias")
+    if wdtype not in _FLOATS:
+        raise TypeError(f"weight must be float32, bfloat16 or float16 (got {wdtype})")
+    return wp, bp, wdtype
+
+
+@_streamed
+def svm_layernorm(x, weight=None, bias=None, eps: float = 1e-5, *, out_dtype=None):
+    """(x - mean) * rstd * weight + bias, row by row; returns (y, mean, rstd), the last two for the gradient.
+    y is of x's type or float32, weight and bias likewise."""
+    lib = load()
+    xtype, ldx = _float_rows(x, "x")
+    n, d = x.shape
+    wp, bp, wdtype = _weight_args(x, weight, bias)
+    y = torch.empty((n, d), dtype=out_dtype or x.dtype, device=x.device)
+    ytype, ldy = _float_rows(y, "y")
+    stats = torch.empty((2, n), dtype=torch.float32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    _check(lib.svm_layernorm(x.data_ptr(), xtype, n, d, ldx, wp, bp, _FLOATS[wdtype], eps, y.data_ptr(), ytype, ldy,
+                             mean.data_ptr(), rstd.data_ptr(), _stream_options()))
+    return y, mean, rstd
+
+
+@_streamed
+def svm_layernorm_grad(dy, x, mean, rstd, weight=None, *, weight_dtype=None):
+    """Gradients (dx, dweight, dbias) of svm_layernorm; dweight and dbias are of the weight's type (without a
+    weight: ``weight_dtype``, default float32)."""
+    lib = load()
+    xtype, ldx = _float_rows(x, "x")
+    n, d = x.shape
+    ytype, ldy = _float_rows(dy, "dy", (n, d))
+    wp, _, wdtype = _weight_args(x, weight, None)
+    if weight is None and weight_dtype is not None:
+        wdtype = weight_dtype
+    dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    dw, db = torch.empty(d, dtype=wdtype, device=x.device), torch.empty(d, dtype=wdtype, device=x.device)
+    ws = _workspace(lib.svm_layernorm_grad_workspace_bytes(n, d, xtype), x.device)
+    _check(lib.svm_layernorm_grad(dy.data_ptr(), ytype, ldy, x.data_ptr(), xtype, n, d, ldx,
+                                  _vector(mean, torch.float32, n, "mean"), _vector(rstd, torch.float32, n, "rstd"), wp,
+                                  _FLOATS[wdtype], dx.data_ptr(), d, dw.data_ptr(), db.data_ptr(), ws.data_ptr(),
+                                  ws.shape[0], _stream_options()))
+    return dx, dw, db
+
+
+ADAMW_BLOCK = 256  # values of one scale of an 8-bit state
+
+
+def svm_adamw_states(params, dtype=torch.float32):
+    """New states for svm_adamw: (m, v, m_scale, v_scale), lists of zeros; the scales are None for float32 states."""
+    m = [torch.zeros(p.numel(), dtype=torch.uint8, device=p.device).view(dtype) if dtype == torch.float8_e4m3fn
+         else torch.zeros(p.numel(), dtype=dtype, device=p.device) for p in params]
+    v = [torch.zeros_like(t.view(torch.uint8)).view(dtype) if dtype == torch.float8_e4m3fn else torch.zeros_like(t) for t in m]
+    if dtype == torch.float32:
+        return m, v, None, None
+    scales = [torch.zeros(-(-p.numel() // ADAMW_BLOCK), dtype=torch.float32, device=p.device) for p in params]
+    return m, v, scales, [torch.zeros_like(s) for s in scales]
+
+
+def _flat(t, types, count, device, name):
+    """Address of a contiguous tensor of one of the types."""
+    if not t.is_cuda or t.get_device() != device:
+        raise TypeError(f"{name} must be on the current device")
+    if t.dtype not in types or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous and one of {[str(k) for k in types]} (got {t.dtype})")
+    if t.numel() != count:
+        raise ValueError(f"{name} must have {count} values (got {t.numel()})")
+    return t.data_ptr()
+
+
+_F32_ONLY = {torch.float32: SVM_F32}
+
+
+@_streamed
+def svm_adamw(params, grads, m, v, step: int, lr: float, *, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+              weight_decay=0.0, grad_scale=1.0, m_scale=None, v_scale=None, master=None) -> None:
+    """One AdamW step over lists of tensors, in place.  States are float32, or float8_e4m3fn with m_scale and
+    v_scale (svm_adamw_states makes them).  ``master``: float32 copies that are updated in the place of 16-bit
+    params, which become their roundings.  ``weight_decay``: one number, or one a tensor.  ``grad_scale``: factor
+    on the gradients, a number or a one-element float32 device tensor (clipping by a norm known on the device)."""
+    lib = load()
+    count = len(params)
+    decay = [float(weight_decay)] * count if not isinstance(weight_decay, (list, tuple)) else weight_decay
+    for name, lst in (("grads", grads), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale), ("master", master),
+                      ("weight_decay", decay)):
+        if lst is not None and len(lst) != count:
+            raise ValueError(f"{name} must have one entry for each of the {count} params")
+    device = torch.cuda.current_device()
+    words = np.zeros((max(count, 1), 11), dtype=np.int64)  # svm_adamw_tensor, 8 bytes a word
+    rows = []
+    for i in range(count):
+        p, g = params[i], grads[i]
+        n = p.numel()
+        f8 = m[i].dtype == torch.float8_e4m3fn
+        if f8 and (m_scale is None or v_scale is None):
+            raise ValueError("float8 states need m_scale and v_scale")
+        blocks = -(-n // ADAMW_BLOCK)
+        rows.append((_flat(p, _FLOATS, n, device, "params"),
+                     0 if master is None or master[i] is None else _flat(master[i], _F32_ONLY, n, device, "master"),
+                     _flat(g, _FLOATS, n, device, "grads"), _flat(m[i], _STATES, n, device, "m"),
+                     _flat(v[i], {m[i].dtype: 0}, n, device, "v"),
+                     _flat(m_scale[i], _F32_ONLY, blocks, device, "m_scale") if f8 else 0,
+                     _flat(v_scale[i], _F32_ONLY, blocks, device, "v_scale") if f8 else 0, n, 0,
+                     _FLOATS[p.dtype] | _FLOATS[g.dtype] << 32, SVM_F8 if f8 else SVM_F32))
+    if count:
+        words[:] = rows
+        words[:, 8] = np.asarray(decay, dtype=np.float64).view(np.int64)
+    a = svm_adamw_params(struct_size=C.sizeof(svm_adamw_params), step=step, lr=lr, beta1=beta1, beta2=beta2, eps=eps,
+                         grad_scale=1.0)
+    if isinstance(grad_scale, torch.Tensor):
+        a.grad_scale_device = _flat(grad_scale, _F32_ONLY, 1, device, "grad_scale")
+    else:
+        a.grad_scale = grad_scale
+    _check(lib.svm_adamw(words.ctypes.data, count, C.byref(a), _stream_options()))
+
+
+def _machine_args(X, y, alpha):
+    for t, dtype, name in ((X, torch.float32, "X"), (y, torch.int32, "y"), (alpha, torch.float64, "alpha")):
+        _on_device(t, name)
+        _dev(t, dtype, name)
+    if X.dim() != 2 or y.shape != (X.shape[0],) or alpha.shape != (X.shape[0],):
+        raise ValueError("X must be [n, d], y and alpha [n]")
+    return X.shape
+
+
+@_streamed
+def svm_predict_grad(X_train, y, alpha, gamma: float, X_test, upstream=None) -> torch.Tensor:
+    """Gradient [m, d] of the decision values (times ``upstream``, float64 [m]) in the test samples."""
+    lib = load()
+    n, d = _machine_args(X_train, y, alpha)
+    _on_device(X_test, "X_test")
+    _dev(X_test, torch.float32, "X_test")
+    if X_test.dim() != 2 or X_test.shape[1] != d:
+        raise ValueError(f"X_test must be [m, {d}] (got {tuple(X_test.shape)})")
+    m = X_test.shape[0]
+    up = None if upstream is None else _vector(upstream, torch.float64, m, "upstream")
+    dX = torch.empty((m, d), dtype=torch.float32, device=X_train.device)
+    ws = _workspace(lib.svm_predict_grad_workspace_bytes(n, d, m), X_train.device)
+    _check(lib.svm_predict_grad(X_train.data_ptr(), y.data_ptr(), alpha.data_ptr(), n, d, gamma, X_test.data_ptr(), m, up,
+                                dX.data_ptr(), _ptr(ws), 0 if ws is None else ws.shape[0], _stream_options()))
+    return dX
+
+
+@_streamed
+def svm_objective_grad(X, y, alpha, gamma: float) -> torch.Tensor:
+    """Gradient [n, d] of the trained machine's objective in its rows."""
+    lib = load()
+    n, d = _machine_args(X, y, alpha)
+    dX = torch.empty((n, d), dtype=torch.float32, device=X.device)
+    ws = _workspace(lib.svm_objective_grad_workspace_bytes(n, d), X.device)
+    _check(lib.svm_objective_grad(X.data_ptr(), y.data_ptr(), alpha.data_ptr(), n, d, gamma, dX.data_ptr(), _ptr(ws),
+                                  0 if ws is None else ws.shape[0], _stream_options()))
+    return dX
