@@ -3,8 +3,21 @@
 // out_q = u_q 2 gamma sum_j c_j K(x_j, x_q) (x_j - x_q), c_j = a_j y_j.  The objective's gradient is the same
 // sum with the rows themselves as samples and u_q = -c_q (a_j y_j a_q y_q K is symmetric, which cancels the
 // 1/2), zero where a_q = 0; the pair j = q adds nothing and is left out.
+// Few samples (GRAD_FEW) take a pass over the training rows.  More take two products in tiles of 128 x 128 on
+// the fp16 matrix cores with fp32 accuracy (split_tile.hpp), around a matrix of weights in HBM:
+//   1. grad_compact_k: the support vectors in index order, their c_j, its largest magnitude;
+//   2. grad_split_k: split rows of the support vectors and of the samples;
+//      grad_transpose_k: the support vectors' rows once more, by feature, scaled by their row's 1 / s_j;
+//   3. grad_weights_k, for as many samples at a time as the workspace holds weights for: p_qj = c_j s_j K_qj,
+//      stored as two fp16 halves each, and sums of c_j K_qj over every 64 support vectors;
+//   4. grad_product_k: p times the rows by feature, over a share of the support vectors;
+//   5. grad_finish_k: the shares' sums, minus (sum c_j K_qj) x_q, times u_q 2 gamma.
+// The weights are scaled to 2^15 and the rows to 2^14 at most before they are split: a half keeps 11 bits
+// only down to 2^-14, and a kernel value of 2^-25 still has all its 22 that way.
 #include "layers.hpp"
 #include "rbf_d2.hpp"
+#include "split_rows.hpp"
+#include "split_tile.hpp"
 #include "units.hpp"
 
 namespace svmx {
@@ -144,15 +157,396 @@ __global__ void __launch_bounds__(GB) sv_grad_join_k(SvGradCall c, int64_t chunk
   store_n<4>(c.out + i, total - i, s);
 }
 
+// ---------------------------------------------------------------------------- tiles
+
+constexpr int TB = 256;               // threads
+constexpr int COMPACT_MAX = 64;       // workgroups of the compaction
+constexpr int W_EXP = 15, X_EXP = 14; // largest weight and row value, as powers of two
+constexpr int64_t WEIGHT_BYTES = 2LL << 30;  // weights held at once
+
+inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+struct GradTiles {
+  int32_t *sv_row;    // [n]
+  float *coef;        // [n]: c_j (fp32)
+  int32_t *count;     // support vectors; [1]: bits of the largest row scale
+  float *cmax;        // [COMPACT_MAX]: largest |c_j| of each workgroup of the compaction
+  int32_t nblocks;    // of them
+  SplitX sv, q;       // split rows (compact; q = sv for the objective's gradient)
+  SplitX xt;          // [d] rows by feature, dp = svp
+  SplitX p;           // [mc] rows of weights, dp = svp
+  float *sums;        // [svp / 64][mc]
+  float *part;        // [splits][mc][dc]
+  int64_t mc, svp, dc;
+  int32_t splits;
+};
+
+// Samples whose weights are held at once, and shares of the support vectors in the second product: about
+// 2,048 workgroups of it (two rounds of what the device holds), 16 shares at most.
+GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
+  GradTiles t{};
+  t.svp = round_up(n, ST);
+  t.dc = round_up(d, 4);
+  const int64_t most = WEIGHT_BYTES / (4 * t.svp) / ST * ST;
+  t.mc = round_up(m, ST);
+  if (t.mc > most) t.mc = most < ST ? ST : most;
+  const int64_t tiles = t.mc / ST * div_up(d, ST), s = 2048 / tiles;
+  t.splits = (int32_t)(s < 1 ? 1 : s > 16 ? 16 : s);
+  t.nblocks = (int32_t)(div_up(n, 1024) > COMPACT_MAX ? COMPACT_MAX : div_up(n, 1024));
+  return t;
+}
+
+// Places everything in ws (NULL: only counts); returns the bytes.
+int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool objective) {
+  const uintptr_t base = (reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255;
+  uintptr_t at = base;
+  const auto take = [&](int64_t bytes) {
+    const uintptr_t p = at;
+    at += (uintptr_t)round_up(bytes, 256);
+    return reinterpret_cast<void *>(p);
+  };
+  t.sv_row = static_cast<int32_t *>(take(4 * n));
+  t.coef = static_cast<float *>(take(4 * n));
+  t.count = static_cast<int32_t *>(take(8));
+  t.cmax = static_cast<float *>(take(4 * COMPACT_MAX));
+  t.sv = split_views(take(gram_split_scratch_bytes(n, d)), n, d);
+  t.q = objective ? t.sv : split_views(take(gram_split_scratch_bytes(m, d)), m, d);
+  t.xt.dp = t.p.dp = t.svp;
+  t.xt.rows = static_cast<_Float16 *>(take(4 * d * t.svp));
+  t.p.rows = static_cast<_Float16 *>(take(4 * t.mc * t.svp));
+  t.sums = static_cast<float *>(take(4 * t.svp / 64 * t.mc));
+  t.part = static_cast<float *>(take(4 * t.splits * t.mc * t.dc));
+  return (int64_t)(at - base) + 256;
+}
+
+// Support vectors in index order (every workgroup counts those before its share itself), their c_j, and the
+// largest |c_j| of the share.
+__global__ void __launch_bounds__(TB) grad_compact_k(SvGradCall c, GradTiles t) {
+  __shared__ int red[TB / 64];
+  __shared__ float top[TB / 64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t chunk = ((c.n + gridDim.x - 1) / gridDim.x + TB - 1) / TB * TB;
+  const int64_t c0 = min(c.n, blockIdx.x * chunk), c1 = min(c.n, c0 + chunk);
+  int before = 0;
+#pragma unroll 16
+  for (int64_t j = threadIdx.x; j < c0; j += TB) before += c.alpha[j] > 0.0 ? 1 : 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
+  if (lane == 0) red[w] = before;
+  __syncthreads();
+  int base = 0;
+#pragma unroll
+  for (int q = 0; q < TB / 64; ++q) base += red[q];
+  __syncthreads();
+  float most = 0.f;
+  for (int64_t j0 = c0; j0 < c1; j0 += TB) {
+    const int64_t j = j0 + threadIdx.x;
+    const double a = j < c1 ? c.alpha[j] : 0.0;
+    const unsigned long long mask = __ballot(a > 0.0);
+    if (lane == 0) red[w] = __popcll(mask);
+    __syncthreads();
+    int off = __popcll(mask & ((1ull << lane) - 1ull)), tot = 0;
+#pragma unroll
+    for (int q = 0; q < TB / 64; ++q) {
+      off += q < w ? red[q] : 0;
+      tot += red[q];
+    }
+    if (a > 0.0) {
+      const float cj = (float)(a * (double)c.y[j]);
+      t.sv_row[base + off] = (int32_t)j;
+      t.coef[base + off] = cj;
+      most = fmaxf(most, fabsf(cj));
+    }
+    base += tot;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+  if (lane == 0) top[w] = most;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  t.cmax[blockIdx.x] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  if (blockIdx.x == gridDim.x - 1) t.count[0] = base;
+  if (blockIdx.x == 0) t.count[1] = 0;
+}
+
+// Split rows of the support vectors (blocks up to sv_blocks) and of the samples; the largest scale of the
+// former (a maximum, so its order does not matter).
+__global__ void __launch_bounds__(TB) grad_split_k(SplitRows sv, SplitRows q, int64_t d, int32_t *__restrict__ count,
+                                                   int32_t sv_blocks) {
+  if ((int)blockIdx.x >= sv_blocks) {
+    split_rows_block(q, d, blockIdx.x - sv_blocks, gridDim.x - sv_blocks, [](int64_t pos) { return pos; });
+    return;
+  }
+  const int64_t nsv = count[0];
+  sv.count = nsv;
+  split_rows_block(sv, d, blockIdx.x, sv_blocks, [](int64_t pos) { return pos; });
+  // this workgroup's own rows again: their scales, just written by lane 0 of each row group
+  const int per = TB / sv.gs, g = threadIdx.x & (sv.gs - 1), mine = threadIdx.x / sv.gs;
+  int most = 0;
+  for (int64_t r = (int64_t)blockIdx.x * per + mine; g == 0 && r < nsv; r += (int64_t)sv_blocks * per)
+    most = max(most, sv.s.nrm[r] < INFINITY ? __float_as_int(sv.s.scale[r]) : 0);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
+  if ((threadIdx.x & 63) == 0 && most > __atomic_load_n(&count[1], __ATOMIC_RELAXED)) atomicMax(&count[1], most);
+}
+
+// Rows by feature: 32 support vectors x 64 features a workgroup, through LDS; past the last support vector zeros.
+__global__ void __launch_bounds__(TB) grad_transpose_k(const float *__restrict__ X, int64_t d, GradTiles t) {
+  __shared__ float v[32][65];
+  const int nsv = t.count[0];
+  const int s0 = blockIdx.x * 32;
+  if (s0 >= (nsv + ST - 1) / ST * ST) return;
+  const int64_t f0 = (int64_t)blockIdx.y * 64;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = threadIdx.x / 64 + 4 * k, f = threadIdx.x % 64;
+    float x = 0.f;
+    if (s0 + r < nsv && f0 + f < d)
+      x = X[(int64_t)t.sv_row[s0 + r] * d + f0 + f] * (1.0f / t.sv.scale[s0 + r]) * (float)(1 << X_EXP);
+    v[r][f] = x;
+  }
+  __syncthreads();
+  // thread: 8 support vectors of one feature
+  const int f = threadIdx.x / 4, r0 = threadIdx.x % 4 * 8;
+  if (f0 + f >= d) return;
+  split_h8 h, l;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = v[r0 + e][f];
+    h[e] = (_Float16)x;
+    l[e] = (_Float16)(x - (float)h[e]);
+  }
+  _Float16 *o = t.xt.rows + (f0 + f) * 2 * t.svp + (int64_t)s0 * 2 + r0;
+  *reinterpret_cast<split_h8 *>(o) = h;
+  *reinterpret_cast<split_h8 *>(o + 32) = l;
+}
+
+__device__ __forceinline__ float wave_most(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// Power of two above the largest |c_j|.
+__device__ __forceinline__ int coef_exp(const GradTiles &t) {
+  const int lane = threadIdx.x & 63;
+  int e = 0;
+  (void)frexpf(wave_most(lane < t.nblocks ? t.cmax[lane] : 0.f), &e);
+  return e;
+}
+
+// Tile i of `tiles`, so that each XCD (workgroup % 8) takes a contiguous share of them.
+__device__ __forceinline__ bool xcd_item(int64_t tiles, int64_t i, int64_t &item) {
+  const int64_t share = (tiles + 7) / 8;
+  item = (i % 8) * share + i / 8;
+  return i / 8 < share && item < tiles;
+}
+
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+
+// Weights of 128 samples x 128 support vectors.  The support vectors are the MFMA's row operand, so a lane
+// holds 4 consecutive ones of a sample and stores 8 bytes of each half.  Tiles in the order (8 tiles of
+// samples) x support vectors.
+__global__ void __launch_bounds__(SBS, 3) grad_weights_k(SvGradCall c, GradTiles t, float cexp, int64_t q_first, int64_t q_end) {
+  __shared__ SplitStage S;
+  __shared__ float sA[ST], nA[ST], cA[ST], sB[ST], nB[ST];
+  const bool objective = c.Q == nullptr;
+  const int nsv = t.count[0];
+  if (objective) q_end = min(q_end, (int64_t)nsv);
+  if (q_first >= q_end || nsv == 0) return;
+  const int64_t nst = (nsv + ST - 1) / ST, nqt = (q_end - q_first + ST - 1) / ST;
+  int64_t item;
+  if (!xcd_item(nst * nqt, blockIdx.x, item)) return;
+  const int64_t sup = item / (8 * nst), rem = item - sup * 8 * nst, wide = min((int64_t)8, nqt - 8 * sup);
+  const int64_t s0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / wide)) * ST;
+  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(8 * sup + rem % wide)) * ST;  // among those held
+  const int64_t q0 = q_first + l0;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
+  const char *src[SCH];
+#pragma unroll
+  for (int q = 0; q < SCH; ++q) {
+    const int i = ((w & 1) * SCH + q) * 8 + (lane >> 3);
+    src[q] = w < 2 ? split_src(t.sv, min<int64_t>(s0 + i, nsv - 1)) : split_src(t.q, min<int64_t>(q0 + i, q_end - 1));
+  }
+  split_stage_load(S, src);
+  const int ec = coef_exp(t);
+  if (threadIdx.x < ST) {
+    const int64_t j = min<int64_t>(s0 + threadIdx.x, nsv - 1), q = min<int64_t>(q0 + threadIdx.x, q_end - 1);
+    const float nj = t.sv.nrm[j], nq = t.q.nrm[q];
+    // a row whose norm overflows has no neighbour but its copies, which add nothing
+    sA[threadIdx.x] = nj < INFINITY ? t.sv.scale[j] : 0.f;
+    nA[threadIdx.x] = nj;
+    cA[threadIdx.x] = s0 + threadIdx.x < nsv && nj < INFINITY ? ldexpf(t.coef[j], -ec) : 0.f;
+    sB[threadIdx.x] = nq < INFINITY ? -2.0f * t.q.scale[q] : 0.f;
+    nB[threadIdx.x] = nq;
+  }
+  int es = 0;
+  (void)frexpf(__int_as_float(t.count[1]), &es);
+  const float norm = ldexpf(1.0f, W_EXP - es);  // s_j norm <= 2^W_EXP
+  v4f acc[4][4];
+  split_tile_loaded(S, src, t.sv.dp / SKS, wm, wn, acc);
+  float sum[4] = {};
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int lr = wm * 64 + a * 16 + 4 * kq;
+    const v4f sa = *reinterpret_cast<const v4f *>(&sA[lr]), na = *reinterpret_cast<const v4f *>(&nA[lr]);
+    const v4f ca = *reinterpret_cast<const v4f *>(&cA[lr]);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int lc = wn * 64 + b * 16 + r16;
+      const float sb = sB[lc], nb = nB[lc];
+      h4 h, l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float d2 = __builtin_fmaf(acc[a][b][e] * sa[e], sb, na[e] + nb);
+        d2 = d2 > 0.f ? d2 : 0.f;
+        float p = ca[e] * __builtin_amdgcn_exp2f(cexp * d2);
+        if (objective && s0 + lr + e == q0 + lc) p = 0.f;
+        sum[b] += p;
+        p *= sa[e] * norm;
+        h[e] = (_Float16)p;
+        l[e] = (_Float16)(p - (float)h[e]);
+      }
+      _Float16 *o = t.p.rows + (l0 + lc) * 2 * t.svp + ((s0 + lr) >> 5) * 64 + (lr & 31);
+      *reinterpret_cast<h4 *>(o) = h;
+      *reinterpret_cast<h4 *>(o + 32) = l;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    sum[b] += __shfl_xor(sum[b], 16);
+    sum[b] += __shfl_xor(sum[b], 32);
+    if (kq == 0) t.sums[(s0 / 64 + wm) * t.mc + l0 + wn * 64 + b * 16 + r16] = sum[b];
+  }
+}
+
+// 128 features x 128 samples of the second product, over one share of the support vectors.  Features are the row
+// operand: a lane holds 4 consecutive ones of a sample.
+__global__ void __launch_bounds__(SBS, 4) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+  __shared__ SplitStage S;
+  const int nsv = t.count[0];
+  if (c.Q == nullptr) q_end = min(q_end, (int64_t)nsv);
+  if (q_first >= q_end || nsv == 0) return;
+  const int64_t nft = (c.d + ST - 1) / ST, nqt = (q_end - q_first + ST - 1) / ST;
+  int64_t item;
+  if (!xcd_item(nft * nqt * t.splits, blockIdx.x, item)) return;
+  const int split = __builtin_amdgcn_readfirstlane((int)(item / (nft * nqt)));
+  const int64_t rem = item - (int64_t)split * nft * nqt;
+  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / nft)) * ST;
+  const int64_t f0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem % nft)) * ST;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
+  const int64_t stages = (nsv + SKS - 1) / SKS, per = (stages + t.splits - 1) / t.splits;
+  const int64_t st0 = min(stages, split * per), st1 = min(stages, st0 + per);
+  v4f acc[4][4];
+  if (st0 < st1) {
+    const char *src[SCH];
+#pragma unroll
+    for (int q = 0; q < SCH; ++q) {
+      const int i = ((w & 1) * SCH + q) * 8 + (lane >> 3);
+      src[q] = (w < 2 ? split_src(t.xt, min<int64_t>(f0 + i, c.d - 1)) : split_src(t.p, l0 + i)) + st0 * 4 * SKS;
+    }
+    split_stage_load(S, src);
+    split_tile_loaded(S, src, st1 - st0, wm, wn, acc);
+  } else {
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
+  }
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int64_t f = f0 + wm * 64 + a * 16 + 4 * kq;
+    if (f >= t.dc) continue;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      *reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l0 + wn * 64 + b * 16 + r16) * t.dc + f]) = acc[a][b];
+  }
+}
+
+// One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x).
+__global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+  const bool objective = c.Q == nullptr;
+  const int nsv = t.count[0], lane = threadIdx.x & 63;
+  if (objective) q_end = min(q_end, (int64_t)nsv);
+  const int64_t l = (int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6), q = q_first + l;
+  if (q >= q_end) return;
+  const int ec = coef_exp(t);
+  int es = 0;
+  (void)frexpf(__int_as_float(t.count[1]), &es);
+  const int64_t row = objective ? t.sv_row[q] : q;
+  const double up = objective ? -(double)t.coef[q] : c.up ? c.up[q] : 1.0;
+  const double f = nsv ? ldexp(2.0 * c.gamma * up, ec) : 0.0;
+  const double scale = ldexp(1.0, es - W_EXP - X_EXP);
+  float s = 0.f;
+  for (int64_t k = lane; k < (nsv + ST - 1) / ST * 2; k += 64) s += t.sums[k * t.mc + l];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  const float *x = (objective ? c.X : c.Q) + row * c.d;
+  for (int64_t at = 4 * lane; at < c.d; at += 256) {
+    float xv[4], o[4] = {};
+    load_n<4>(x + at, c.d - at, xv);
+    for (int k = 0; nsv && k < t.splits; ++k) {
+      const v4f v = *reinterpret_cast<const v4f *>(&t.part[((int64_t)k * t.mc + l) * t.dc + at]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - (double)s * (double)xv[e]));
+    store_n<4>(c.out + row * c.d + at, c.d - at, o);
+  }
+}
+
+// The objective's gradient: zeros in the rows that are no support vectors.
+__global__ void __launch_bounds__(TB) grad_zero_k(SvGradCall c) {
+  const int64_t q = (int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6);
+  if (q >= c.m || c.alpha[q] > 0.0) return;
+  const float z[4] = {};
+  for (int64_t at = 4 * (threadIdx.x & 63); at < c.d; at += 256) store_n<4>(c.out + q * c.d + at, c.d - at, z);
+}
+
+constexpr int64_t GRAD_FEW = 16;  // samples that take the pass
+
+hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
+  const bool objective = c.Q == nullptr;
+  GradTiles t = tile_plan(c.n, c.d, c.m);
+  tile_views(t, ws, c.n, c.d, c.m, objective);
+  hipLaunchKernelGGL(grad_compact_k, dim3((unsigned)t.nblocks), dim3(TB), 0, s, c, t);
+  SplitRows sv = split_rows_of(c.X, c.n, t.sv), q = split_rows_of(objective ? c.X : c.Q, objective ? 0 : c.m, t.q);
+  sv.perm = t.sv_row;
+  const int64_t svb = split_rows_blocks(sv), qb = split_rows_blocks(q);
+  hipLaunchKernelGGL(grad_split_k, dim3((unsigned)(svb + qb)), dim3(TB), 0, s, sv, q, c.d, t.count, (int32_t)svb);
+  if (div_up(c.d, 64) > 65535) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(grad_transpose_k, dim3((unsigned)(t.svp / 32), (unsigned)div_up(c.d, 64)), dim3(TB), 0, s, c.X, c.d, t);
+  if (objective) hipLaunchKernelGGL(grad_zero_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c);
+  const float cexp = (float)(-c.gamma * 1.4426950408889634);
+  for (int64_t q0 = 0; q0 < c.m; q0 += t.mc) {
+    const int64_t q1 = c.m - q0 < t.mc ? c.m : q0 + t.mc, nqt = div_up(q1 - q0, ST);
+    const int64_t wb = round_up(nqt * (t.svp / ST), 8), pb = round_up(nqt * div_up(c.d, ST) * t.splits, 8);
+    if (wb > 0x7fffffffLL || pb > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(grad_weights_k, dim3((unsigned)wb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
+    hipLaunchKernelGGL(grad_product_k, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t, q0, q1);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
-int64_t sv_grad_scratch_bytes(int64_t n, int64_t d, int64_t m, bool) {
+int64_t sv_grad_scratch_bytes(int64_t n, int64_t d, int64_t m, bool objective) {
   if (m == 0) return 0;
+  if (m > GRAD_FEW) {
+    GradTiles t = tile_plan(n, d, m);
+    return tile_views(t, nullptr, n, d, m, objective);
+  }
   const int64_t chunks = grad_chunks(n, d, m);
   return chunks == 1 ? 0 : 4 * chunks * m * d + 256;
 }
 
 hipError_t launch_sv_grad(const SvGradCall &c, void *ws, hipStream_t s) {
+  if (c.m > GRAD_FEW) return launch_tiles(c, ws, s);
   const int64_t chunks = grad_chunks(c.n, c.d, c.m), groups = div_up(c.m, GQ);
   float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
   hipLaunchKernelGGL(sv_grad_k, dim3((unsigned)groups, (unsigned)div_up(c.d, 4 * GB), (unsigned)chunks), dim3(GB), 0, s, c,
