@@ -17,10 +17,13 @@ namespace svmx {
 
 namespace {
 
-constexpr int EB = 256;           // threads of a workgroup
-constexpr int EU = 8;             // rows of a thread on their way at once
+constexpr int EB = 256;             // threads of a workgroup
+constexpr int EU = 8;               // rows of a thread on their way at once
 constexpr int64_t RANK_MAX = 8192;  // positions sorted by counting smaller ones
+constexpr int SB = 512;             // threads of a workgroup of the sort
 constexpr int SORT_BLOCKS = 256;
+constexpr int DIGIT_MAX = 9;        // bits of a pass of the sort at most
+constexpr int SPAN = 32;            // chunks of a run that one thread joins
 
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -58,6 +61,45 @@ __device__ __forceinline__ int64_t bag_at(const EmbedCall &c, int64_t i) {
   return b < 0 ? 0 : b >= c.B ? c.B - 1 : b;
 }
 
+// The part of a row a thread holds: N values from column `at`.  Where d is no multiple of N the last unit ends at
+// the row's end and overlaps the one before by `skip` values, which it computes but does not write, so
+// every load is a whole one; rows shorter than a unit (SMALL) are read value by value.
+template <int N, bool SMALL>
+struct Columns {
+  int64_t at, left;
+  int skip;
+  __device__ __forceinline__ Columns(int64_t unit, int64_t d) {
+    at = SMALL ? 0 : min(unit * N, d - N);
+    left = SMALL ? d : N;
+    skip = SMALL ? 0 : (int)(unit * N - at);
+  }
+  template <class T>
+  __device__ __forceinline__ Raw<N, T> load(const T *__restrict__ row) const {
+    if (SMALL) return load_raw<N>(row + at, left);
+    return load_whole<N>(row + at);
+  }
+  __device__ __forceinline__ void store(void *p, int32_t type, int64_t row_at, const float (&v)[N]) const {
+    if (skip == 0)
+      store_any<N>(p, type, row_at + at, left, v);
+    else
+#pragma unroll
+      for (int e = 1; e < N; ++e) {
+        const float one[1] = {v[e]};
+        if (e >= skip) store_any<1>(p, type, row_at + at + e, 1, one);
+      }
+  }
+  // with `accumulate`, added to what is there
+  __device__ __forceinline__ void put(void *p, int32_t type, int64_t row_at, bool accumulate, float (&v)[N]) const {
+    if (accumulate) {
+      float old[N];
+      load_any<N>(p, type, row_at + at, left, old);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] += old[e];
+    }
+    store(p, type, row_at, v);
+  }
+};
+
 // Item of this thread: `of` = which chunk or row, `unit` = which 16 bytes of it.
 __device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &unit) {
   const int64_t b0 = (int64_t)blockIdx.x * EB, c0 = b0 / units;
@@ -66,26 +108,33 @@ __device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &uni
   unit = r % (uint32_t)units;
 }
 
-// Sum of E[token] over positions lo .. hi - 1, EU rows on their way at once; `used` counts positions that
-// are not padding.  A token outside the table reads nothing and makes the sum NaN.
-template <int N, class TE>
+// Sum of E[token] over positions lo .. hi - 1, EU rows on their way at once, the next EU tokens ahead of them;
+// `used` counts positions that are not padding.  A token outside the table reads nothing and makes the sum NaN.
+template <int N, bool SMALL, class TE>
 __device__ __forceinline__ void sum_tokens(const EmbedCall &c, const TE *__restrict__ E, int64_t ld, int64_t lo, int64_t hi,
-                                           int64_t at, int64_t left, float (&acc)[N], int &used) {
+                                           const Columns<N, SMALL> &col, float (&acc)[N], int &used) {
+  if (lo >= hi) return;
+  int64_t t[EU];
+#pragma unroll
+  for (int q = 0; q < EU; ++q) t[q] = token_at(c, min(lo + q, hi - 1));
   for (int64_t i = lo; i < hi; i += EU) {
-    float v[EU][N];
+    Raw<N, TE> v[EU];
     bool live[EU], bad[EU];
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
-      const int64_t t = i + q < hi ? token_at(c, i + q) : 0;
-      live[q] = i + q < hi && (c.padding < 0 || t != c.padding);
-      bad[q] = live[q] && (t < 0 || t >= c.V);
-      load_n<N>(E + (live[q] && !bad[q] ? t : 0) * ld + at, left, v[q]);
+      live[q] = i + q < hi && (c.padding < 0 || t[q] != c.padding);
+      bad[q] = live[q] && (t[q] < 0 || t[q] >= c.V);
+      v[q] = col.load(E + (live[q] && !bad[q] ? t[q] : 0) * ld);
+    }
+    if (i + EU < hi) {
+#pragma unroll
+      for (int q = 0; q < EU; ++q) t[q] = token_at(c, min(i + EU + q, hi - 1));
     }
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
       used += live[q] ? 1 : 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += bad[q] ? __builtin_nanf("") : live[q] ? v[q][e] : 0.f;
+      for (int e = 0; e < N; ++e) acc[e] += bad[q] ? __builtin_nanf("") : live[q] ? v[q].at(e) : 0.f;
     }
   }
 }
@@ -95,35 +144,45 @@ __device__ __forceinline__ float bag_weight(const EmbedCall &c, int64_t used) {
 }
 
 // A row a position (no bags).
-template <int N, class TE>
+template <int N, bool SMALL, class TE>
 __global__ void __launch_bounds__(EB) embed_rows_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
                                                    int32_t out_type, int64_t ld_out, int64_t units) {
   int64_t row, unit;
   item_of(units, row, unit);
   if (row >= c.T) return;
-  const int64_t at = unit * N, left = c.d - at, t = token_at(c, row);
+  const Columns<N, SMALL> col(unit, c.d);
+  const int64_t t = token_at(c, row);
   const bool pad = c.padding >= 0 && t == c.padding, bad = !pad && (t < 0 || t >= c.V);
+  const Raw<N, TE> r = col.load(E + (pad || bad ? 0 : t) * ld);
   float v[N];
-  load_n<N>(E + (pad || bad ? 0 : t) * ld + at, left, v);
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = bad ? __builtin_nanf("") : pad ? 0.f : v[e] * c.scale;
-  store_any<N>(out, out_type, row * ld_out + at, left, v);
+  for (int e = 0; e < N; ++e) v[e] = bad ? __builtin_nanf("") : pad ? 0.f : r.at(e) * c.scale;
+  col.store(out, out_type, row * ld_out, v);
 }
+
+// Partial sums of the runs that cross an end of their chunk: [chunk][0: the run began before it, 1: it goes on
+// after it][units x N].
+struct Parts {
+  float *sum;
+  int32_t *used;  // forward: the positions that count, [chunk][2]
+  int32_t *tail;  // forward: the bag that begins in the chunk and goes on after it, or -1
+};
 
 // One unit of one chunk of positions (see the top).  A bag belongs to the chunk that holds its start; an
 // empty one at the very end to the last chunk.
-template <int N, class TE>
+template <int N, bool SMALL, class TE>
 __global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
                                                    int32_t out_type, int64_t ld_out, int64_t units, int64_t L,
-                                                   int64_t chunks, float *__restrict__ part, int32_t *__restrict__ pcount) {
+                                                   int64_t chunks, Parts part) {
   int64_t ch, unit;
   item_of(units, ch, unit);
   if (ch >= chunks) return;
-  const int64_t at = unit * N, left = c.d - at, dp = units * N;
+  const Columns<N, SMALL> col(unit, c.d);
   const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
   int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i0);
   bool head = b > c.B || c.bags[b] != i0;
   if (head) --b;
+  int32_t tail = -1;
   for (; b >= 0 && b < c.B; ++b, head = false) {
     const int64_t s0 = c.bags[b], s1 = c.bags[b + 1];
     if (!head && s0 >= i1 && i1 < c.T) break;
@@ -132,41 +191,54 @@ __global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__rest
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
     int used = 0;
-    sum_tokens<N>(c, E, ld, lo, hi, at, left, acc, used);
+    sum_tokens<N, SMALL>(c, E, ld, lo, hi, col, acc, used);
     const bool more = s1 > i1 && i1 < c.T;
     if (head || more) {
       const int64_t p = ch * 2 + (head ? 0 : 1);
-      store_n<N>(part + p * dp + at, N, acc);
-      if (unit == 0) pcount[p] = used;
+      store_n<N>(part.sum + (p * units + unit) * N, N, acc);
+      if (unit == 0) part.used[p] = used;
+      if (!head) tail = (int32_t)b;
     } else {
       const float w = bag_weight(c, used);
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] *= w;
-      store_any<N>(out, out_type, b * ld_out + at, left, acc);
+      col.store(out, out_type, b * ld_out, acc);
     }
     if (more) break;
   }
+  if (unit == 0) part.tail[ch] = tail;
 }
 
-constexpr int JU = 16, JS = EB / JU;  // a join: units side by side, slices of the chunks
+constexpr int JU = 16, JS = EB / JU;  // the join of a long run: units side by side, slices of its chunks
 
-// acc = the tail of chunk ch and the heads of chunks ch + 1 .. last, in slices joined in order; valid in the
-// threads of slice 0.
+// acc = the tail of chunk ch and the heads of chunks ch + 1 .. last of one unit, in order.
 template <int N>
-__device__ __forceinline__ void join_parts(const float *__restrict__ part, int64_t dp, int64_t at, bool in, int64_t ch,
-                                           int64_t last, float (&acc)[N], float (*lds)[JU][N]) {
+__device__ __forceinline__ void join_short(const float *__restrict__ part, int64_t units, int64_t unit, int64_t ch,
+                                           int64_t last, float (&acc)[N]) {
+  load_n<N>(part + ((ch * 2 + 1) * units + unit) * N, N, acc);
+#pragma unroll 8
+  for (int64_t k = ch + 1; k <= last; ++k) {
+    const Raw<N, float> v = load_whole<N>(part + (k * 2 * units + unit) * N);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] += v.at(e);
+  }
+}
+
+// The same by a workgroup, 16 slices of the chunks joined in order; valid in the threads of slice 0.
+template <int N>
+__device__ __forceinline__ void join_long(const float *__restrict__ part, int64_t units, int64_t unit, int64_t ch,
+                                          int64_t last, float (&acc)[N], float (*lds)[JU][N]) {
   const int u = threadIdx.x % JU, sl = threadIdx.x / JU;
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  if (in) {
+  if (unit < units) {
     const int64_t count = last - ch + 1, per = (count + JS - 1) / JS;
     const int64_t k1 = min(count, (sl + 1) * per);
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t k = sl * per; k < k1; ++k) {
-      float v[N];
-      load_n<N>(part + ((ch + k) * 2 + (k == 0 ? 1 : 0)) * dp + at, N, v);
+      const Raw<N, float> v = load_whole<N>(part + (((ch + k) * 2 + (k == 0 ? 1 : 0)) * units + unit) * N);
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += v[e];
+      for (int e = 0; e < N; ++e) acc[e] += v.at(e);
     }
   }
 #pragma unroll
@@ -178,38 +250,56 @@ __device__ __forceinline__ void join_parts(const float *__restrict__ part, int64
       for (int e = 0; e < N; ++e) acc[e] += lds[k][u][e];
 }
 
-// Workgroup (x, y): the bag that starts in chunk x and goes on past its end, if there is one; units 16 y ..
-template <int N>
+// Runs that cross an end of a chunk.  Blocks up to `short_blocks`: a thread for each unit of each chunk in which
+// such a run begins, if it spans up to SPAN chunks.  The blocks after them: one for each 16 units and each
+// SPAN-th chunk, which joins the run that reaches this chunk from before, if it spans more and no
+// earlier such chunk has it.
+template <int N, bool SMALL>
 __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32_t out_type, int64_t ld_out, int64_t units,
-                                                   int64_t L, const float *__restrict__ part,
-                                                   const int32_t *__restrict__ pcount) {
+                                                   int64_t L, int64_t chunks, int64_t short_blocks, Parts part) {
   __shared__ float lds[JS][JU][N];
   __shared__ int counts[EB / 64];
-  const int64_t ch = blockIdx.x, i0 = ch * L, i1 = min(c.T, i0 + L);
-  if (i1 >= c.T) return;
-  const int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i1) - 1;
-  if (b < 0 || b >= c.B || c.bags[b] < i0 || c.bags[b + 1] <= i1) return;
-  const int64_t last = (min(c.bags[b + 1], c.T) - 1) / L;
-  const int64_t unit = (int64_t)blockIdx.y * JU + threadIdx.x % JU, at = unit * N;
-  int used = 0;
-  for (int64_t k = threadIdx.x; k <= last - ch; k += EB) used += pcount[(ch + k) * 2 + (k == 0 ? 1 : 0)];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) used += __shfl_xor(used, o);
-  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = used;
+  int64_t ch, unit, b, last;
   float acc[N];
-  join_parts<N>(part, units * N, at, unit < units, ch, last, acc, lds);
-  if (threadIdx.x >= JU || unit >= units) return;
-  const float w = bag_weight(c, counts[0] + counts[1] + counts[2] + counts[3]);
+  int used = 0;
+  if ((int64_t)blockIdx.x < short_blocks) {
+    item_of(units, ch, unit);
+    if (ch >= chunks) return;
+    b = part.tail[ch];
+    if (b < 0) return;
+    last = (min(c.bags[b + 1], c.T) - 1) / L;
+    if (last - ch >= SPAN) return;
+    join_short<N>(part.sum, units, unit, ch, last, acc);
+    used = part.used[ch * 2 + 1];
+    for (int64_t k = ch + 1; k <= last; ++k) used += part.used[k * 2];
+  } else {
+    const int64_t i = blockIdx.x - short_blocks, groups = (units + JU - 1) / JU, x = (i / groups + 1) * SPAN;
+    if (x >= chunks) return;
+    b = lower_bound<int64_t>(c.bags, c.B + 1, x * L) - 1;
+    if (b < 0 || b >= c.B || c.bags[b] < 0 || c.bags[b + 1] <= x * L) return;
+    ch = c.bags[b] / L;
+    last = (min(c.bags[b + 1], c.T) - 1) / L;
+    if (last - ch < SPAN || ch < x - SPAN) return;
+    unit = i % groups * JU + threadIdx.x % JU;
+    for (int64_t k = threadIdx.x; k <= last - ch; k += EB) used += part.used[(ch + k) * 2 + (k == 0 ? 1 : 0)];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) used += __shfl_xor(used, o);
+    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = used;
+    join_long<N>(part.sum, units, unit, ch, last, acc, lds);
+    if (threadIdx.x >= JU || unit >= units) return;
+    used = counts[0] + counts[1] + counts[2] + counts[3];
+  }
+  const float w = bag_weight(c, used);
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] *= w;
-  store_any<N>(out, out_type, b * ld_out + at, c.d - at, acc);
+  Columns<N, SMALL>(unit, c.d).store(out, out_type, b * ld_out, acc);
 }
 
 // ---------------------------------------------------------------------------- gradient
 
 struct GradSpace {
   uint32_t *key[2], *src[2];  // [T]: token (V: none) and bag, before and after a pass of the sort
-  uint32_t *hist;             // [SORT_BLOCKS][256]
+  uint32_t *hist;             // [SORT_BLOCKS][2^DIGIT_MAX]
   int32_t *count;             // [B]: positions of a bag that count (mean)
   float *part;                // [chunks][2][d padded]
 };
@@ -226,7 +316,7 @@ GradSpace grad_views(void *ws, int64_t T, int64_t B) {
     g.key[k] = reinterpret_cast<uint32_t *>(take(4 * T));
     g.src[k] = reinterpret_cast<uint32_t *>(take(4 * T));
   }
-  g.hist = reinterpret_cast<uint32_t *>(take(4LL * SORT_BLOCKS * 256));
+  g.hist = reinterpret_cast<uint32_t *>(take(4LL * SORT_BLOCKS << DIGIT_MAX));
   g.count = reinterpret_cast<int32_t *>(take(4 * B));
   g.part = reinterpret_cast<float *>(p);
   return g;
@@ -275,7 +365,7 @@ __device__ __forceinline__ void zero_rows(void *de, int32_t type, int64_t rows, 
   const float z[N] = {};
   for (int64_t r = 0; r < rows; ++r) {
     if (rows > 1 && r % blocks != blk) continue;
-    for (int64_t u = (rows > 1 ? 0 : blk * EB) + threadIdx.x; u < units; u += rows > 1 ? EB : blocks * EB)
+    for (int64_t u = (rows > 1 ? 0 : blk * blockDim.x) + threadIdx.x; u < units; u += rows > 1 ? blockDim.x : blocks * blockDim.x)
       store_any<N>(de, type, r * ld + u * N, d - u * N, z);
   }
 }
@@ -287,93 +377,128 @@ struct FillCall {
 };
 
 // Up to RANK_MAX positions: the place of a position is the number of positions with a smaller token, or the
-// same token and a smaller index.  64 positions a workgroup, a quarter of the comparisons a wave.  Blocks
-// past those zero dE meanwhile.
+// same token and a smaller index.  16 positions a workgroup, and 16 threads a position that take every
+// 16th four of the others, so the LDS reads of a wave's four slices are one after the other in memory.
+// Blocks past the sort's zero dE meanwhile.
+constexpr int RP = 16, RS = EB / RP;
+
 __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks) {
   if ((int64_t)blockIdx.x >= sort_blocks) {
     zero_rows(f.de, f.type, f.rows, f.d, f.ld, blockIdx.x - sort_blocks, f.blocks);
     return;
   }
   extern __shared__ uint32_t keys[];
-  __shared__ int ranks[EB / 64][64];
-  const int T = (int)c.T, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int Tp = (T + 15) / 16 * 16;
-  for (int j = threadIdx.x; j < Tp; j += EB) keys[j] = j < T ? key_at(c, j) : 0xffffffffu;
+  __shared__ int ranks[RS][RP], counts[RS][RP];
+  const int T = (int)c.T, pos = threadIdx.x % RP, sl = threadIdx.x / RP;
+  const int Tp = (T + 4 * RS - 1) / (4 * RS) * (4 * RS);
+  for (int j0 = threadIdx.x; j0 < Tp; j0 += 8 * EB) {
+    uint32_t k[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {  // (V: padding; V + 1: outside the table)
+      const int j = j0 + q * EB;
+      const int64_t t = token_at(c, min(j, T - 1));
+      k[q] = c.padding >= 0 && t == c.padding ? (uint32_t)c.V : t < 0 || t >= c.V ? (uint32_t)c.V + 1 : (uint32_t)t;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (j0 + q * EB < Tp) keys[j0 + q * EB] = j0 + q * EB < T ? k[q] : 0xffffffffu;
+  }
+  const int p0 = blockIdx.x * RP, i = p0 + pos;
+  const int64_t b = bag_at(c, min(i, T - 1));
+  int64_t s0 = 0, s1 = 0;
+  if (c.mean && c.bags) {
+    s0 = c.bags[b];
+    s1 = min(c.bags[b + 1], c.T);
+  }
   __syncthreads();
-  const int p0 = blockIdx.x * 64, i = p0 + lane;
   const uint32_t k = i < T ? keys[i] : 0u;
-  const int quarter = Tp / 4;
-  const int j0 = w * quarter, j1 = j0 + quarter;
   int rank = 0;
-  for (int j = j0; j < j1; j += 4) {
+#pragma unroll 4
+  for (int j = 4 * sl; j < Tp; j += 4 * RS) {
     const uint4 o = *reinterpret_cast<const uint4 *>(&keys[j]);
     if (j + 4 <= p0) {
       rank += (o.x <= k) + (o.y <= k) + (o.z <= k) + (o.w <= k);
-    } else if (j >= p0 + 64) {
+    } else if (j >= p0 + RP) {
       rank += (o.x < k) + (o.y < k) + (o.z < k) + (o.w < k);
     } else {
       rank += (o.x < k || (o.x == k && j < i)) + (o.y < k || (o.y == k && j + 1 < i)) +
               (o.z < k || (o.z == k && j + 2 < i)) + (o.w < k || (o.w == k && j + 3 < i));
     }
   }
-  ranks[w][lane] = rank;
+  ranks[sl][pos] = rank;
+  // the first position of a bag counts the bag's that are not padding
+  int used = 0;
+  if (i < T && i == s0)
+    for (int64_t j = s0 + sl; j < s1; j += RS) used += c.padding < 0 || keys[j] != (uint32_t)c.V ? 1 : 0;
+  counts[sl][pos] = used;
   __syncthreads();
-  if (w != 0 || i >= T) return;
-  rank = ranks[0][lane] + ranks[1][lane] + ranks[2][lane] + ranks[3][lane];
-  const int64_t b = bag_at(c, i);
-  g.key[0][rank] = k;
+  if (sl != 0 || i >= T) return;
+  rank = used = 0;
+#pragma unroll
+  for (int q = 0; q < RS; ++q) {
+    rank += ranks[q][pos];
+    used += counts[q][pos];
+  }
+  g.key[0][rank] = min(k, (uint32_t)c.V);
   g.src[0][rank] = (uint32_t)b;
-  if (c.mean && c.bags) count_position(c, i, b, g.count);
+  if (c.mean && c.bags && i == s0) g.count[b] = used;
 }
 
-// More positions: a stable radix sort, 8 bits a pass.  Block b holds `per` consecutive positions.  This
-// kernel makes keys and bags and counts the first digit of every block; blocks past the sort's zero dE.
-__global__ void __launch_bounds__(EB) embed_expand_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks, int64_t per) {
+// More positions: a stable radix sort, `bits` bits a pass (two passes up to 2^18 tokens).  Block b holds `per`
+// consecutive positions.  This kernel makes keys and bags and counts the first digit of every block; blocks
+// past the sort's zero dE.
+__global__ void __launch_bounds__(SB) embed_expand_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks, int64_t per,
+                                                     int bits) {
   if ((int64_t)blockIdx.x >= sort_blocks) {
     zero_rows(f.de, f.type, f.rows, f.d, f.ld, blockIdx.x - sort_blocks, f.blocks);
     return;
   }
-  __shared__ uint32_t h[256];
+  __shared__ uint32_t h[1 << DIGIT_MAX];
+  static_assert(SB == 1 << DIGIT_MAX, "a thread a digit");
+  const uint32_t mask = (1u << bits) - 1u;
   h[threadIdx.x] = 0;
   __syncthreads();
   const int64_t i1 = min(c.T, (blockIdx.x + 1) * per);
-  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += EB) {
+  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += SB) {
     const uint32_t k = key_at(c, i);
     const int64_t b = bag_at(c, i);
     g.key[0][i] = k;
     g.src[0][i] = (uint32_t)b;
     if (c.mean && c.bags) count_position(c, i, b, g.count);
-    atomicAdd(&h[k & 255], 1u);
+    atomicAdd(&h[k & mask], 1u);
   }
   __syncthreads();
-  g.hist[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
+  g.hist[((int64_t)blockIdx.x << DIGIT_MAX) + threadIdx.x] = h[threadIdx.x];
 }
 
-__global__ void __launch_bounds__(EB) radix_count_k(const uint32_t *__restrict__ key, int64_t T, int shift, int64_t per,
-                                                    uint32_t *__restrict__ hist) {
-  __shared__ uint32_t h[256];
+__global__ void __launch_bounds__(SB) radix_count_k(const uint32_t *__restrict__ key, int64_t T, int shift, int bits,
+                                                    int64_t per, uint32_t *__restrict__ hist) {
+  __shared__ uint32_t h[1 << DIGIT_MAX];
+  const uint32_t mask = (1u << bits) - 1u;
   h[threadIdx.x] = 0;
   __syncthreads();
   const int64_t i1 = min(T, (blockIdx.x + 1) * per);
-  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += EB) atomicAdd(&h[(key[i] >> shift) & 255], 1u);
+  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += SB) atomicAdd(&h[(key[i] >> shift) & mask], 1u);
   __syncthreads();
-  hist[blockIdx.x * 256 + threadIdx.x] = h[threadIdx.x];
+  hist[((int64_t)blockIdx.x << DIGIT_MAX) + threadIdx.x] = h[threadIdx.x];
 }
 
 // Every position of this block to its place: the positions with a smaller digit, those with its digit in
-// blocks before, and those before it in this block, 256 of them at a time (a wave counts its own by
+// blocks before, and those before it in this block, 512 of them at a time (a wave counts its own by
 // ballots over the digit's bits).
-__global__ void __launch_bounds__(EB) radix_place_k(const uint32_t *__restrict__ key, const uint32_t *__restrict__ src,
+__global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__ key, const uint32_t *__restrict__ src,
                                                     uint32_t *__restrict__ key_out, uint32_t *__restrict__ src_out,
-                                                    int64_t T, int shift, int64_t per, const uint32_t *__restrict__ hist) {
-  __shared__ uint32_t base[256];          // next place of each digit
-  __shared__ uint32_t wave_n[EB / 64][256];
-  __shared__ uint32_t wsum[EB / 64];
+                                                    int64_t T, int shift, int bits, int64_t per,
+                                                    const uint32_t *__restrict__ hist) {
+  __shared__ uint32_t base[SB];  // next place of each digit
+  __shared__ uint32_t wave_n[SB / 64][SB];
+  __shared__ uint32_t wsum[SB / 64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const uint32_t dmask = (1u << bits) - 1u;
   uint32_t before = 0, total = 0;
-#pragma unroll 16
+#pragma unroll 32
   for (int b = 0; b < (int)gridDim.x; ++b) {
-    const uint32_t v = hist[b * 256 + t];
+    const uint32_t v = hist[(b << DIGIT_MAX) + t];
     before += b < (int)blockIdx.x ? v : 0;
     total += v;
   }
@@ -389,17 +514,17 @@ __global__ void __launch_bounds__(EB) radix_place_k(const uint32_t *__restrict__
   for (int q = 0; q < w; ++q) b0 += wsum[q];
   base[t] = b0;
 #pragma unroll
-  for (int q = 0; q < EB / 64; ++q) wave_n[q][t] = 0;
+  for (int q = 0; q < SB / 64; ++q) wave_n[q][t] = 0;
   __syncthreads();
   const int64_t i0 = blockIdx.x * per, i1 = min(T, i0 + per);
-  for (int64_t r = i0; r < i1; r += EB) {
+  for (int64_t r = i0; r < i1; r += SB) {
     const int64_t i = r + t;
     const bool in = i < i1;
-    const uint32_t k = in ? key[i] : 0, dig = (k >> shift) & 255;
+    const uint32_t k = in ? key[i] : 0, dig = (k >> shift) & dmask;
     const uint32_t s = in ? src[i] : 0;
     unsigned long long same = __ballot(in);
 #pragma unroll
-    for (int bit = 0; bit < 8; ++bit) {
+    for (int bit = 0; bit < DIGIT_MAX; ++bit) {
       const unsigned long long m = __ballot(in && ((dig >> bit) & 1));
       same &= (dig >> bit) & 1 ? m : ~m;
     }
@@ -415,7 +540,7 @@ __global__ void __launch_bounds__(EB) radix_place_k(const uint32_t *__restrict__
     __syncthreads();
     uint32_t add = 0;
 #pragma unroll
-    for (int q = 0; q < EB / 64; ++q) {
+    for (int q = 0; q < SB / 64; ++q) {
       add += wave_n[q][t];
       wave_n[q][t] = 0;
     }
@@ -424,19 +549,8 @@ __global__ void __launch_bounds__(EB) radix_place_k(const uint32_t *__restrict__
   }
 }
 
-template <int N>
-__device__ __forceinline__ void put_row(void *de, int32_t type, int64_t at, int64_t left, bool accumulate, float (&acc)[N]) {
-  if (accumulate) {
-    float old[N];
-    load_any<N>(de, type, at, left, old);
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] += old[e];
-  }
-  store_any<N>(de, type, at, left, acc);
-}
-
 // One unit of one chunk of the sorted positions (see the top).
-template <int N, class TY>
+template <int N, bool SMALL, class TY>
 __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *__restrict__ key,
                                                    const uint32_t *__restrict__ src, const int32_t *__restrict__ count,
                                                    const TY *__restrict__ dy, int64_t ld, void *de, int32_t de_type,
@@ -445,7 +559,7 @@ __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *
   int64_t ch, unit;
   item_of(units, ch, unit);
   if (ch >= chunks) return;
-  const int64_t at = unit * N, left = c.d - at, dp = units * N;
+  const Columns<N, SMALL> col(unit, c.d);
   const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
   uint32_t run = key[i0];
   bool head = i0 > 0 && key[i0 - 1] == run;  // the run began before this chunk
@@ -453,58 +567,91 @@ __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
   const bool mean = c.mean && c.bags;
+  uint32_t k[EU], b[EU];
+#pragma unroll
+  for (int q = 0; q < EU; ++q) {
+    const int64_t j = min(i0 + q, i1 - 1);
+    k[q] = key[j];
+    b[q] = src[j];
+  }
   for (int64_t i = i0; i < i1 && run < (uint32_t)c.V; i += EU) {
-    float v[EU][N], wt[EU];
-    uint32_t k[EU];
+    Raw<N, TY> v[EU];
+    float wt[EU];
+    uint32_t now[EU];
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
-      const int64_t j = min(i + q, i1 - 1);
-      k[q] = key[j];
-      const int64_t b = src[j];
-      wt[q] = mean ? c.scale / (float)count[b] : c.scale;
-      load_n<N>(dy + b * ld + at, left, v[q]);
+      v[q] = col.load(dy + (int64_t)b[q] * ld);
+      wt[q] = mean ? (float)count[b[q]] : 1.f;
+      now[q] = k[q];
+    }
+    if (i + EU < i1) {
+#pragma unroll
+      for (int q = 0; q < EU; ++q) {
+        const int64_t j = min(i + EU + q, i1 - 1);
+        k[q] = key[j];
+        b[q] = src[j];
+      }
     }
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
       if (i + q >= i1) break;
-      if (k[q] != run) {
+      if (now[q] != run) {
         if (head)
-          store_n<N>(part + ch * 2 * dp + at, N, acc);
+          store_n<N>(part + (ch * 2 * units + unit) * N, N, acc);
         else if (run < (uint32_t)c.V)
-          put_row<N>(de, de_type, run * ld_de + at, left, accumulate, acc);
+          col.put(de, de_type, run * ld_de, accumulate, acc);
         head = false;
-        run = k[q];
+        run = now[q];
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
       }
+      const float w = mean ? c.scale / wt[q] : c.scale;
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = __builtin_fmaf(wt[q], v[q][e], acc[e]);
+      for (int e = 0; e < N; ++e) acc[e] = __builtin_fmaf(w, v[q].at(e), acc[e]);
     }
   }
   if (run >= (uint32_t)c.V) return;
   const bool more = i1 < c.T && key[i1] == run;
   if (head || more)
-    store_n<N>(part + (ch * 2 + (head ? 0 : 1)) * dp + at, N, acc);
+    store_n<N>(part + ((ch * 2 + (head ? 0 : 1)) * units + unit) * N, N, acc);
   else
-    put_row<N>(de, de_type, run * ld_de + at, left, accumulate, acc);
+    col.put(de, de_type, run * ld_de, accumulate, acc);
 }
 
-// Workgroup (x, y): the token whose run starts in chunk x and goes on past its end, if there is one.
-template <int N>
+// Runs of a token that cross an end of a chunk, as embed_join_k.
+template <int N, bool SMALL>
 __global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint32_t *__restrict__ key, void *de,
                                                         int32_t de_type, int64_t ld_de, int32_t accumulate,
-                                                        int64_t units, int64_t L, const float *__restrict__ part) {
+                                                        int64_t units, int64_t L, int64_t chunks, int64_t short_blocks,
+                                                        const float *__restrict__ part) {
   __shared__ float lds[JS][JU][N];
-  const int64_t ch = blockIdx.x, i0 = ch * L, i1 = min(c.T, i0 + L);
-  if (i1 >= c.T) return;
-  const uint32_t run = key[i1];
-  if (run >= (uint32_t)c.V || key[i1 - 1] != run || (i0 > 0 && key[i0 - 1] == run)) return;
-  const int64_t end = i1 + lower_bound<uint32_t>(key + i1, c.T - i1, run + 1);
-  const int64_t unit = (int64_t)blockIdx.y * JU + threadIdx.x % JU, at = unit * N;
+  int64_t ch, unit;
+  uint32_t run;
   float acc[N];
-  join_parts<N>(part, units * N, at, unit < units, ch, (end - 1) / L, acc, lds);
-  if (threadIdx.x >= JU || unit >= units) return;
-  put_row<N>(de, de_type, run * ld_de + at, c.d - at, accumulate, acc);
+  if ((int64_t)blockIdx.x < short_blocks) {
+    item_of(units, ch, unit);
+    const int64_t i0 = ch * L, i1 = i0 + L;
+    if (ch >= chunks || i1 >= c.T) return;
+    run = key[i1];
+    if (run >= (uint32_t)c.V || key[i1 - 1] != run || (i0 > 0 && key[i0 - 1] == run)) return;
+    // the first chunk whose end the run does not reach
+    int64_t last = ch + 1;
+    while (last - ch < SPAN && (last + 1) * L < c.T && key[(last + 1) * L - 1] == run && key[(last + 1) * L] == run) ++last;
+    if (last - ch >= SPAN) return;
+    join_short<N>(part, units, unit, ch, last, acc);
+  } else {
+    const int64_t i = blockIdx.x - short_blocks, groups = (units + JU - 1) / JU, x = (i / groups + 1) * SPAN;
+    if (x >= chunks) return;
+    run = key[x * L];
+    if (run >= (uint32_t)c.V || key[x * L - 1] != run) return;
+    ch = lower_bound<uint32_t>(key, x * L, run) / L;
+    const int64_t last = (x * L + lower_bound<uint32_t>(key + x * L, c.T - x * L, run + 1) - 1) / L;
+    if (last - ch < SPAN || ch < x - SPAN) return;
+    unit = i % groups * JU + threadIdx.x % JU;
+    join_long<N>(part, units, unit, ch, last, acc, lds);
+    if (threadIdx.x >= JU || unit >= units) return;
+  }
+  Columns<N, SMALL>(unit, c.d).put(de, de_type, run * ld_de, accumulate, acc);
 }
 
 __global__ void __launch_bounds__(EB) embed_check_k(EmbedCall c, int32_t *__restrict__ invalid) {
@@ -523,22 +670,39 @@ __global__ void __launch_bounds__(EB) embed_check_k(EmbedCall c, int32_t *__rest
   if (bad) *invalid = 1;
 }
 
+template <class T, class F>
+hipError_t by_width(int64_t d, F f) {
+  if (d < UNIT<T>) return f((const T *)nullptr, std::true_type{});
+  return f((const T *)nullptr, std::false_type{});
+}
+
+// f(tag of the type, whether rows are shorter than a unit of it)
 template <class F>
-hipError_t by_type(int32_t type, F f) {
-  if (type == SVM_F32) return f((const float *)nullptr);
-  if (type == SVM_BF16) return f((const __bf16 *)nullptr);
-  return f((const _Float16 *)nullptr);
+hipError_t by_type(int32_t type, int64_t d, F f) {
+  if (type == SVM_F32) return by_width<float>(d, f);
+  return type == SVM_BF16 ? by_width<__bf16>(d, f) : by_width<_Float16>(d, f);
 }
 
 bool grid_fits(int64_t blocks) { return blocks <= 0x7fffffffLL; }
 
 int64_t part_floats(int64_t T, int64_t d) { return div_up(T > 0 ? T : 1, chunk_of(T, d)) * 2 * div_up(d, 8) * 8; }
 
+// Blocks of a join: those for short runs, and all.
+void join_blocks(int64_t chunks, int64_t units, int64_t &shorts, int64_t &all) {
+  shorts = div_up(chunks * units, EB);
+  all = shorts + (chunks - 1) / SPAN * div_up(units, JU);
+}
+
+template <class P>
+P *aligned(void *ws) {
+  return reinterpret_cast<P *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+}
+
 }  // namespace
 
 int64_t embed_scratch_bytes(int64_t T, int64_t d, int64_t, bool bags) {
   if (!bags) return 0;
-  return 4 * part_floats(T, d) + 8 * div_up(T > 0 ? T : 1, chunk_of(T, d)) + 512;
+  return 4 * part_floats(T, d) + 12 * div_up(T > 0 ? T : 1, chunk_of(T, d)) + 512;
 }
 
 hipError_t launch_embed_check(const EmbedCall &c, int32_t *invalid, hipStream_t s) {
@@ -551,35 +715,39 @@ hipError_t launch_embed_check(const EmbedCall &c, int32_t *invalid, hipStream_t 
 hipError_t launch_embed(const EmbedCall &c, const void *table, int32_t table_type, int64_t ld_table, void *out,
                         int32_t out_type, int64_t ld_out, void *ws, hipStream_t s) {
   if (c.B <= 0) return hipSuccess;
-  return by_type(table_type, [&](auto *tag) -> hipError_t {
+  return by_type(table_type, c.d, [&](auto *tag, auto small) -> hipError_t {
     using TE = std::remove_cv_t<std::remove_pointer_t<decltype(tag)>>;
     constexpr int N = UNIT<TE>;
+    constexpr bool SMALL = decltype(small)::value;
     const TE *E = static_cast<const TE *>(table);
     const int64_t units = div_up(c.d, N);
     if (!c.bags) {
       const int64_t blocks = div_up(c.T * units, EB);
       if (!grid_fits(blocks)) return hipErrorInvalidValue;
-      hipLaunchKernelGGL((embed_rows_k<N, TE>), dim3((unsigned)blocks), dim3(EB), 0, s, c, E, ld_table, out, out_type,
+      hipLaunchKernelGGL((embed_rows_k<N, SMALL, TE>), dim3((unsigned)blocks), dim3(EB), 0, s, c, E, ld_table, out, out_type,
                          ld_out, units);
       return hipGetLastError();
     }
     const int64_t L = chunk_of(c.T, c.d), chunks = c.T > 0 ? div_up(c.T, L) : 1;
-    const int64_t blocks = div_up(chunks * units, EB);
-    if (!grid_fits(blocks) || div_up(units, JU) > 65535) return hipErrorInvalidValue;
-    float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-    int32_t *pcount = reinterpret_cast<int32_t *>(part + chunks * 2 * units * N);
-    hipLaunchKernelGGL((embed_bags_k<N, TE>), dim3((unsigned)blocks), dim3(EB), 0, s, c, E, ld_table, out, out_type, ld_out,
-                       units, L, chunks, part, pcount);
+    int64_t shorts, all;
+    join_blocks(chunks, units, shorts, all);
+    if (!grid_fits(all)) return hipErrorInvalidValue;
+    Parts part;
+    part.sum = aligned<float>(ws);
+    part.used = reinterpret_cast<int32_t *>(part.sum + chunks * 2 * units * N);
+    part.tail = part.used + 2 * chunks;
+    hipLaunchKernelGGL((embed_bags_k<N, SMALL, TE>), dim3((unsigned)shorts), dim3(EB), 0, s, c, E, ld_table, out, out_type,
+                       ld_out, units, L, chunks, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks == 1) return e;
-    hipLaunchKernelGGL((embed_join_k<N>), dim3((unsigned)chunks, (unsigned)div_up(units, JU)), dim3(EB), 0, s, c, out,
-                       out_type, ld_out, units, L, part, pcount);
+    hipLaunchKernelGGL((embed_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, out, out_type, ld_out, units, L,
+                       chunks, shorts, part);
     return hipGetLastError();
   });
 }
 
 int64_t embed_grad_scratch_bytes(int64_t T, int64_t d, int64_t B) {
-  return 16 * T + 4LL * SORT_BLOCKS * 256 + 4 * B + 4 * part_floats(T, d) + 8 * 256;
+  return 16 * T + (4LL * SORT_BLOCKS << DIGIT_MAX) + 4 * B + 4 * part_floats(T, d) + 8 * 256;
 }
 
 hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type, int64_t ld_dy, void *de,
@@ -590,42 +758,47 @@ hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type
     const int64_t units = ld_de == c.d ? div_up(c.V * c.d, 8 * EB) : c.V;
     f.blocks = units > 2048 ? 2048 : units;
   }
-  const bool counted = c.mean && c.bags && c.padding >= 0 && c.T > 0;
-  if (counted) hipLaunchKernelGGL(zero_counts_k, dim3((unsigned)div_up(c.B, EB)), dim3(EB), 0, s, g.count, c.B);
   int cur = 0;
   if (c.T <= RANK_MAX) {
-    const int64_t blocks = div_up(c.T, 64);
+    const int64_t blocks = div_up(c.T, RP);
     if (blocks + f.blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL(embed_rank_k, dim3((unsigned)(blocks + f.blocks)), dim3(EB), (size_t)div_up(c.T, 16) * 64, s, c, g, f,
-                       blocks);
+    hipLaunchKernelGGL(embed_rank_k, dim3((unsigned)(blocks + f.blocks)), dim3(EB), (size_t)div_up(c.T, 4 * RS) * 16 * RS, s,
+                       c, g, f, blocks);
   } else {
+    if (c.mean && c.bags && c.padding >= 0)
+      hipLaunchKernelGGL(zero_counts_k, dim3((unsigned)div_up(c.B, EB)), dim3(EB), 0, s, g.count, c.B);
     const int64_t want = div_up(c.T, 2048), nb0 = want > SORT_BLOCKS ? SORT_BLOCKS : want;
-    const int64_t per = div_up(div_up(c.T, nb0), EB) * EB, nb = div_up(c.T, per);
-    hipLaunchKernelGGL(embed_expand_k, dim3((unsigned)(nb + f.blocks)), dim3(EB), 0, s, c, g, f, nb, per);
-    int bits = 0;
-    while (bits < 32 && (c.V >> bits) > 0) bits += 8;  // the keys are 0 .. V
-    for (int shift = 0; shift < bits; shift += 8) {
-      if (shift > 0)
-        hipLaunchKernelGGL(radix_count_k, dim3((unsigned)nb), dim3(EB), 0, s, g.key[cur], c.T, shift, per, g.hist);
-      hipLaunchKernelGGL(radix_place_k, dim3((unsigned)nb), dim3(EB), 0, s, g.key[cur], g.src[cur], g.key[1 - cur],
-                         g.src[1 - cur], c.T, shift, per, g.hist);
+    const int64_t per = div_up(div_up(c.T, nb0), SB) * SB, nb = div_up(c.T, per);
+    int width = 1;
+    while ((c.V >> width) > 0) ++width;  // the keys are 0 .. V
+    const int passes = (int)div_up(width, DIGIT_MAX), bits = (int)div_up(width, passes);
+    hipLaunchKernelGGL(embed_expand_k, dim3((unsigned)(nb + f.blocks)), dim3(SB), 0, s, c, g, f, nb, per, bits);
+    for (int pass = 0; pass < passes; ++pass) {
+      const int shift = pass * bits;
+      if (pass > 0)
+        hipLaunchKernelGGL(radix_count_k, dim3((unsigned)nb), dim3(SB), 0, s, g.key[cur], c.T, shift, bits, per, g.hist);
+      hipLaunchKernelGGL(radix_place_k, dim3((unsigned)nb), dim3(SB), 0, s, g.key[cur], g.src[cur], g.key[1 - cur],
+                         g.src[1 - cur], c.T, shift, bits, per, g.hist);
       cur = 1 - cur;
     }
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || c.T == 0) return e;
-  return by_type(dy_type, [&](auto *tag) -> hipError_t {
+  return by_type(dy_type, c.d, [&](auto *tag, auto small) -> hipError_t {
     using TY = std::remove_cv_t<std::remove_pointer_t<decltype(tag)>>;
     constexpr int N = UNIT<TY>;
+    constexpr bool SMALL = decltype(small)::value;
     const int64_t units = div_up(c.d, N), L = chunk_of(c.T, c.d), chunks = div_up(c.T, L);
-    const int64_t blocks = div_up(chunks * units, EB);
-    if (!grid_fits(blocks) || div_up(units, JU) > 65535) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((embed_runs_k<N, TY>), dim3((unsigned)blocks), dim3(EB), 0, s, c, g.key[cur], g.src[cur], g.count,
-                       static_cast<const TY *>(dy), ld_dy, de, de_type, ld_de, accumulate ? 1 : 0, units, L, chunks, g.part);
+    int64_t shorts, all;
+    join_blocks(chunks, units, shorts, all);
+    if (!grid_fits(all)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((embed_runs_k<N, SMALL, TY>), dim3((unsigned)shorts), dim3(EB), 0, s, c, g.key[cur], g.src[cur],
+                       g.count, static_cast<const TY *>(dy), ld_dy, de, de_type, ld_de, accumulate ? 1 : 0, units, L, chunks,
+                       g.part);
     hipError_t e2 = hipGetLastError();
     if (e2 != hipSuccess || chunks == 1) return e2;
-    hipLaunchKernelGGL((embed_runs_join_k<N>), dim3((unsigned)chunks, (unsigned)div_up(units, JU)), dim3(EB), 0, s, c,
-                       g.key[cur], de, de_type, ld_de, accumulate ? 1 : 0, units, L, g.part);
+    hipLaunchKernelGGL((embed_runs_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, g.key[cur], de, de_type, ld_de,
+                       accumulate ? 1 : 0, units, L, chunks, shorts, g.part);
     return hipGetLastError();
   });
 }

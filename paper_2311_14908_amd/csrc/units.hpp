@@ -18,6 +18,33 @@ struct VecOf {
   typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
+// N values as they were read (converted where they are used, so that several loads can be under way).
+template <int N, class T>
+struct Raw {
+  static constexpr int M = N < UNIT<T> ? N : UNIT<T>;
+  typename VecOf<T, M>::type v[N / M];
+  __device__ __forceinline__ float at(int e) const { return (float)v[e / M][e % M]; }
+};
+
+template <int N, class T>
+__device__ __forceinline__ Raw<N, T> load_whole(const T *__restrict__ p) {
+  Raw<N, T> r;
+#pragma unroll
+  for (int q = 0; q < N / Raw<N, T>::M; ++q)
+    r.v[q] = *reinterpret_cast<const typename VecOf<T, Raw<N, T>::M>::type *>(p + q * Raw<N, T>::M);
+  return r;
+}
+
+// Of which `left` are in the row; the others come as 0.
+template <int N, class T>
+__device__ __forceinline__ Raw<N, T> load_raw(const T *__restrict__ p, int64_t left) {
+  if (left >= N) return load_whole<N>(p);
+  Raw<N, T> r;
+#pragma unroll
+  for (int e = 0; e < N; ++e) r.v[e / Raw<N, T>::M][e % Raw<N, T>::M] = e < left ? p[e] : (T)0.f;
+  return r;
+}
+
 // N values at p, of which `left` are in the row; the others come as 0.
 template <int N, class T>
 __device__ __forceinline__ void load_n(const T *__restrict__ p, int64_t left, float (&v)[N]) {
