@@ -3,7 +3,7 @@
 // out_q = u_q 2 gamma sum_j c_j K(x_j, x_q) (x_j - x_q), c_j = a_j y_j.  The objective's gradient is the same
 // sum with the rows themselves as samples and u_q = -c_q (a_j y_j a_q y_q K is symmetric, which cancels the
 // 1/2), zero where a_q = 0; the pair j = q adds nothing and is left out.
-// Few samples (GRAD_FEW) take a pass over the training rows.  More take two products in tiles of 128 x 128 on
+// Up to 16 samples of up to 1,024 features take a pass over the training rows.  More take two products in tiles of 128 x 128 on
 // the fp16 matrix cores with fp32 accuracy (split_tile.hpp), around a matrix of weights in HBM:
 //   1. grad_compact_k: the support vectors in index order, their c_j, its largest magnitude;
 //   2. grad_split_k: split rows of the support vectors and of the samples;
@@ -24,46 +24,48 @@ namespace svmx {
 
 namespace {
 
-constexpr int GB = 256, GQ = 4, GL = 256;  // threads, samples of a workgroup, rows looked at in one go
-
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Chunks of training rows: about 1,024 workgroups in all, 64 rows a chunk at least.
-int64_t grad_chunks(int64_t n, int64_t d, int64_t m) {
-  const int64_t wide = div_up(m, GQ) * div_up(d, 4 * GB), most = div_up(n, 64);
-  const int64_t c = wide >= 1024 ? 1 : 1024 / wide;
-  return c > most ? most : c > 256 ? 256 : c;
+constexpr int GB = 256, GU = 4;  // threads, units of four features a lane holds of a row
+constexpr int GL = 256;          // training rows looked at in one go
+constexpr int64_t FEW_M = 16, FEW_D = 4LL * GU * 64;  // samples and features the pass takes
+
+// Chunks of training rows: 32 rows each, at most 512 of them.
+int64_t few_chunks(int64_t n) {
+  const int64_t c = div_up(n, 32);
+  return c > 512 ? 512 : c;
 }
 
-// Workgroup (x, y, z): samples 4 x .., columns 1024 y .., chunk z of the training rows.  The chunk's support
-// vectors are listed in LDS 256 rows at a time; a wave takes one after the other, adds up the squared
-// differences of the four samples in fp64 and leaves c K; then the threads, a unit of four columns each,
-// add c K (x_j - x_q) over the listed rows.
-__global__ void __launch_bounds__(GB) sv_grad_k(SvGradCall c, double cexp, int64_t chunks, float *__restrict__ part) {
+// Workgroup (x, y): chunk x of the training rows, samples MQ y ..  The chunk's support vectors are listed in LDS;
+// gs lanes of a wave take one after the other and hold its row (the next one is on its way), the samples and
+// the sums: the squared differences are added in fp64, then c K (x_j - x_q) is added where it stands, so a
+// row is read once.  The differences are exact or nearly so, and nothing cancels afterwards.
+template <int MQ>
+__global__ void __launch_bounds__(GB) sv_grad_few_k(SvGradCall c, double cexp, int gs, int64_t per, int64_t dc,
+                                                    float *__restrict__ part) {
   __shared__ int32_t rows[GL];
   __shared__ double coefs[GL];
-  __shared__ float wt[GL][GQ];
   __shared__ int cnt[GB / 64];
+  extern __shared__ float sums[];  // [row groups][dc]
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int g = threadIdx.x & (gs - 1), grp = threadIdx.x / gs, groups = GB / gs;
   const bool objective = c.Q == nullptr;
   const float *Q = objective ? c.X : c.Q;
-  const int64_t q0 = (int64_t)blockIdx.x * GQ, at = ((int64_t)blockIdx.y * GB + threadIdx.x) * 4;
-  const int64_t per = (c.n + chunks - 1) / chunks, j1 = min(c.n, (blockIdx.z + 1) * per);
-  const float *t[GQ];
-  double up[GQ];
-  bool any = false;
+  const int64_t q0 = (int64_t)blockIdx.y * MQ;
+  const int64_t c0 = blockIdx.x * per, c1 = min(c.n, c0 + per);
+  float t[MQ][GU][4], acc[MQ][GU][4];
 #pragma unroll
-  for (int q = 0; q < GQ; ++q) {
-    const int64_t i = min(q0 + q, c.m - 1);
-    t[q] = Q + i * c.d;
-    const double a = objective ? c.alpha[i] : 0.0;
-    up[q] = objective ? (a > 0.0 ? -a * (double)c.y[i] : 0.0) : c.up ? c.up[i] : 1.0;
-    any = any || !objective || a > 0.0;
-  }
-  float acc[GQ][4] = {};
-  for (int64_t j0 = blockIdx.z * per; any && j0 < j1; j0 += GL) {
+  for (int q = 0; q < MQ; ++q)
+#pragma unroll
+    for (int i = 0; i < GU; ++i) {
+      const int64_t at = 4 * (int64_t)(g + i * gs);
+      load_n<4>(Q + min(q0 + q, c.m - 1) * c.d + at, c.d - at, t[q][i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[q][i][e] = 0.f;
+    }
+  for (int64_t j0 = c0; j0 < c1; j0 += GL) {
     const int64_t j = j0 + threadIdx.x;
-    const double a = j < j1 ? c.alpha[j] : 0.0;
+    const double a = j < c1 ? c.alpha[j] : 0.0;
     const unsigned long long mask = __ballot(a > 0.0);
     if (lane == 0) cnt[w] = __popcll(mask);
     __syncthreads();
@@ -78,89 +80,122 @@ __global__ void __launch_bounds__(GB) sv_grad_k(SvGradCall c, double cexp, int64
       coefs[off] = a * (double)c.y[j];
     }
     __syncthreads();
-    for (int r = w; r < nsv; r += GB / 64) {
-      const float *x = c.X + (int64_t)rows[r] * c.d;
-      double s[GQ] = {};
-      for (int64_t k = 4 * lane; k < c.d; k += 256) {
-        float xv[4];
-        load_n<4>(x + k, c.d - k, xv);
+    float x[GU][4], nx[GU][4];
+    const auto fetch = [&](int r, float (&o)[GU][4]) {
+      const float *p = c.X + (int64_t)rows[r] * c.d;
 #pragma unroll
-        for (int q = 0; q < GQ; ++q) {
-          float tv[4];
-          load_n<4>(t[q] + k, c.d - k, tv);
+      for (int i = 0; i < GU; ++i) {
+        const int64_t at = 4 * (int64_t)(g + i * gs);
+        load_n<4>(p + at, c.d - at, o[i]);
+      }
+    };
+    if (grp < nsv) fetch(grp, nx);
+    for (int r = grp; r < nsv; r += groups) {  // (a row group is inside one wave)
+#pragma unroll
+      for (int i = 0; i < GU; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = nx[i][e];
+      if (r + groups < nsv) fetch(r + groups, nx);
+      double s[MQ];
+#pragma unroll
+      for (int q = 0; q < MQ; ++q) {
+        s[q] = 0.0;
+#pragma unroll
+        for (int i = 0; i < GU; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const double f = (double)(xv[e] - tv[e]);
+            const double f = (double)(x[i][e] - t[q][i][e]);
             s[q] = __builtin_fma(f, f, s[q]);
           }
-        }
       }
+      for (int o = gs >> 1; o > 0; o >>= 1)
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1)
+        for (int q = 0; q < MQ; ++q) s[q] += __shfl_xor(s[q], o);
 #pragma unroll
-        for (int q = 0; q < GQ; ++q) s[q] += __shfl_xor(s[q], o);
-      if (lane < GQ) {
-        double d2 = s[0];
+      for (int q = 0; q < MQ; ++q) {
+        const float wt = objective && q0 + q == rows[r] ? 0.f : (float)(coefs[r] * rbf_of_d2(cexp, s[q]));
 #pragma unroll
-        for (int q = 1; q < GQ; ++q) d2 = lane == q ? s[q] : d2;
-        wt[r][lane] = objective && q0 + lane == rows[r] ? 0.f : (float)(coefs[r] * rbf_of_d2(cexp, d2));
-      }
-    }
-    __syncthreads();
-    if (at < c.d) {
-      float tv[GQ][4];
+        for (int i = 0; i < GU; ++i)
 #pragma unroll
-      for (int q = 0; q < GQ; ++q) load_n<4>(t[q] + at, c.d - at, tv[q]);
-#pragma unroll 4
-      for (int r = 0; r < nsv; ++r) {
-        float xv[4];
-        load_n<4>(c.X + (int64_t)rows[r] * c.d + at, c.d - at, xv);
-#pragma unroll
-        for (int q = 0; q < GQ; ++q)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[q][e] = __builtin_fmaf(wt[r][q], xv[e] - tv[q][e], acc[q][e]);
+          for (int e = 0; e < 4; ++e) acc[q][i][e] = __builtin_fmaf(wt, x[i][e] - t[q][i][e], acc[q][i][e]);
       }
     }
-    __syncthreads();
+    __syncthreads();  // rows, coefs and cnt are rewritten
   }
-  if (at >= c.d) return;
 #pragma unroll
-  for (int q = 0; q < GQ; ++q) {
-    if (q0 + q >= c.m) break;
-    const float f = chunks == 1 ? (float)(2.0 * c.gamma * up[q]) : 1.f;
+  for (int q = 0; q < MQ; ++q) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[q][e] *= f;
-    float *o = chunks == 1 ? c.out + (q0 + q) * c.d : part + ((int64_t)blockIdx.z * c.m + q0 + q) * c.d;
-    store_n<4>(o + at, c.d - at, acc[q]);
+    for (int i = 0; i < GU; ++i) {
+      const int64_t at = 4 * (int64_t)(g + i * gs);
+      if (at < dc) store_n<4>(&sums[grp * dc + at], 4, acc[q][i]);
+    }
+    __syncthreads();
+    for (int64_t u = threadIdx.x; 4 * u < dc && q0 + q < c.m; u += GB) {
+      float s[4] = {};
+      for (int k = 0; k < groups; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += sums[k * dc + 4 * u + e];
+      store_n<4>(part + ((int64_t)blockIdx.x * c.m + q0 + q) * dc + 4 * u, 4, s);
+    }
+    __syncthreads();
   }
 }
 
-// The chunks' sums in their order, times u_q 2 gamma.
-__global__ void __launch_bounds__(GB) sv_grad_join_k(SvGradCall c, int64_t chunks, const float *__restrict__ part) {
-  const int64_t i = ((int64_t)blockIdx.x * GB + threadIdx.x) * 4, total = c.m * c.d;
-  if (i >= total) return;
+// The chunks' sums in 16 slices joined in order, times u_q 2 gamma.  Workgroup (x, y): units 16 x .., sample y.
+__global__ void __launch_bounds__(GB) sv_grad_few_join_k(SvGradCall c, int64_t chunks, int64_t dc,
+                                                         const float *__restrict__ part) {
+  __shared__ float lds[16][16][4];
+  const int u = threadIdx.x & 15, sl = threadIdx.x >> 4;
+  const int64_t q = blockIdx.y, at = ((int64_t)blockIdx.x * 16 + u) * 4;
+  const int64_t per = (chunks + 15) / 16, k1 = min(chunks, (sl + 1) * per);
   float s[4] = {};
+  if (at < dc) {
 #pragma unroll 8
-  for (int64_t k = 0; k < chunks; ++k) {
-    float v[4];
-    load_n<4>(part + k * total + i, total - i, v);
+    for (int64_t k = sl * per; k < k1; ++k) {
+      float v[4];
+      load_n<4>(part + (k * c.m + q) * dc + at, 4, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += v[e];
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) lds[sl][u][e] = s[e];
+  __syncthreads();
+  if (sl != 0 || at >= c.d) return;
+  const double a = c.Q ? 0.0 : c.alpha[q];
+  const double up = c.Q ? (c.up ? c.up[q] : 1.0) : (a > 0.0 ? -a * (double)c.y[q] : 0.0);
+  const float f = (float)(2.0 * c.gamma * up);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const int64_t q = min((i + e) / c.d, c.m - 1);
-    const double a = c.Q ? 0.0 : c.alpha[q];
-    const double up = c.Q ? (c.up ? c.up[q] : 1.0) : (a > 0.0 ? -a * (double)c.y[q] : 0.0);
-    s[e] *= (float)(2.0 * c.gamma * up);
+    for (int k = 1; k < 16; ++k) s[e] += lds[k][u][e];
+    s[e] = a > 0.0 || c.Q ? s[e] * f : 0.f;
   }
-  store_n<4>(c.out + i, total - i, s);
+  store_n<4>(c.out + q * c.d + at, c.d - at, s);
+}
+
+bool takes_pass(int64_t d, int64_t m) { return m <= FEW_M && d <= FEW_D; }
+
+hipError_t launch_few(const SvGradCall &c, void *ws, hipStream_t s) {
+  const int64_t chunks = few_chunks(c.n), per = div_up(c.n, chunks), dc = div_up(c.d, 4) * 4;
+  float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
+  int gs = 1;
+  while (gs < 64 && 4LL * GU * gs < c.d) gs <<= 1;
+  const size_t lds = (size_t)(GB / gs) * dc * 4;
+  const double cexp = -c.gamma * 1.4426950408889634;
+  const dim3 grid((unsigned)chunks, (unsigned)(c.m == 1 ? 1 : div_up(c.m, 4)));
+  if (c.m == 1)
+    hipLaunchKernelGGL(sv_grad_few_k<1>, grid, dim3(GB), lds, s, c, cexp, gs, per, dc, part);
+  else
+    hipLaunchKernelGGL(sv_grad_few_k<4>, grid, dim3(GB), lds, s, c, cexp, gs, per, dc, part);
+  hipLaunchKernelGGL(sv_grad_few_join_k, dim3((unsigned)div_up(dc, 64), (unsigned)c.m), dim3(GB), 0, s, c, chunks, dc, part);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------- tiles
 
 constexpr int TB = 256;               // threads
 constexpr int COMPACT_MAX = 64;       // workgroups of the compaction
+constexpr int FOLD = 128;             // stages (of 32 support vectors) that one fp32 accumulator sums
 constexpr int W_EXP = 15, X_EXP = 14; // largest weight and row value, as powers of two
 constexpr int64_t WEIGHT_BYTES = 2LL << 30;  // weights held at once
 
@@ -440,30 +475,39 @@ __global__ void __launch_bounds__(SBS, 4) grad_product_k(SvGradCall c, GradTiles
   const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
   const int64_t stages = (nsv + SKS - 1) / SKS, per = (stages + t.splits - 1) / t.splits;
   const int64_t st0 = min(stages, split * per), st1 = min(stages, st0 + per);
-  v4f acc[4][4];
+  const char *src[SCH];
   if (st0 < st1) {
-    const char *src[SCH];
 #pragma unroll
     for (int q = 0; q < SCH; ++q) {
       const int i = ((w & 1) * SCH + q) * 8 + (lane >> 3);
       src[q] = (w < 2 ? split_src(t.xt, min<int64_t>(f0 + i, c.d - 1)) : split_src(t.p, l0 + i)) + st0 * 4 * SKS;
     }
     split_stage_load(S, src);
-    split_tile_loaded(S, src, st1 - st0, wm, wn, acc);
-  } else {
-#pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-      for (int b = 0; b < 4; ++b) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
   }
+  // A sum over 15,000 support vectors is 1,400 roundings of a growing fp32 one after the other; cut every FOLD
+  // stages it is a tenth of that, and the rest happens once a cut (the tile of sums stays in L2 between).
+  int64_t st = st0;
+  do {
+    v4f acc[4][4];
+    const int64_t more = min(st1 - st, (int64_t)FOLD);
+    if (more > 0) {
+      split_tile_loaded(S, src, more, wm, wn, acc);
+      if (st + more < st1) split_stage_load(S, src);
+    }
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    const int64_t f = f0 + wm * 64 + a * 16 + 4 * kq;
-    if (f >= t.dc) continue;
+    for (int a = 0; a < 4; ++a) {
+      const int64_t f = f0 + wm * 64 + a * 16 + 4 * kq;
+      if (f >= t.dc) continue;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
-      *reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l0 + wn * 64 + b * 16 + r16) * t.dc + f]) = acc[a][b];
-  }
+      for (int b = 0; b < 4; ++b) {
+        v4f *o = reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l0 + wn * 64 + b * 16 + r16) * t.dc + f]);
+        if (more <= 0) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
+        if (st > st0) acc[a][b] += *o;
+        *o = acc[a][b];
+      }
+    }
+    st += FOLD;
+  } while (st < st1);
 }
 
 // One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x).
@@ -507,8 +551,6 @@ __global__ void __launch_bounds__(TB) grad_zero_k(SvGradCall c) {
   for (int64_t at = 4 * (threadIdx.x & 63); at < c.d; at += 256) store_n<4>(c.out + q * c.d + at, c.d - at, z);
 }
 
-constexpr int64_t GRAD_FEW = 16;  // samples that take the pass
-
 hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   const bool objective = c.Q == nullptr;
   GradTiles t = tile_plan(c.n, c.d, c.m);
@@ -537,27 +579,13 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
 
 int64_t sv_grad_scratch_bytes(int64_t n, int64_t d, int64_t m, bool objective) {
   if (m == 0) return 0;
-  if (m > GRAD_FEW) {
-    GradTiles t = tile_plan(n, d, m);
-    return tile_views(t, nullptr, n, d, m, objective);
-  }
-  const int64_t chunks = grad_chunks(n, d, m);
-  return chunks == 1 ? 0 : 4 * chunks * m * d + 256;
+  if (takes_pass(d, m)) return 4 * few_chunks(n) * m * div_up(d, 4) * 4 + 256;
+  GradTiles t = tile_plan(n, d, m);
+  return tile_views(t, nullptr, n, d, m, objective);
 }
 
 hipError_t launch_sv_grad(const SvGradCall &c, void *ws, hipStream_t s) {
-  if (c.m > GRAD_FEW) return launch_tiles(c, ws, s);
-  const int64_t chunks = grad_chunks(c.n, c.d, c.m), groups = div_up(c.m, GQ);
-  float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-  hipLaunchKernelGGL(sv_grad_k, dim3((unsigned)groups, (unsigned)div_up(c.d, 4 * GB), (unsigned)chunks), dim3(GB), 0, s, c,
-                     -c.gamma * 1.4426950408889634, chunks, part);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (chunks > 1) {
-    hipLaunchKernelGGL(sv_grad_join_k, dim3((unsigned)div_up(c.m * c.d, 4 * GB)), dim3(GB), 0, s, c, chunks, part);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  return takes_pass(c.d, c.m) ? launch_few(c, ws, s) : launch_tiles(c, ws, s);
 }
 
 }  // namespace svmx
