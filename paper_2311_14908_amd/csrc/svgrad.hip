@@ -194,7 +194,8 @@ hipError_t launch_few(const SvGradCall &c, void *ws, hipStream_t s) {
 // ---------------------------------------------------------------------------- tiles
 
 constexpr int TB = 256;               // threads
-constexpr int COMPACT_MAX = 64;       // workgroups of the compaction
+constexpr int CB = 1024;              // threads of the compaction
+constexpr int COMPACT_MAX = 64;       // and its workgroups
 constexpr int FOLD = 128;             // stages (of 32 support vectors) that one fp32 accumulator sums
 constexpr int W_EXP = 15, X_EXP = 14; // largest weight and row value, as powers of two
 constexpr int64_t WEIGHT_BYTES = 2LL << 30;  // weights held at once
@@ -210,26 +211,42 @@ struct GradTiles {
   SplitX sv, q;       // split rows (compact; q = sv for the objective's gradient)
   SplitX xt;          // [d] rows by feature, dp = svp
   SplitX p;           // [mc] rows of weights, dp = svp
-  float *sums;        // [svp / 64][mc]
+  float *sums;        // [svp / 64][mc]; short rows: [splits][mc]
   float *part;        // [splits][mc][dc]
+  char *image;        // short rows: [svp / 32] blocks (grad_pack_k)
   int64_t mc, svp, dc;
   int32_t splits;
+  int32_t fb;         // short rows: blocks of 16 features; 0: two products around weights in HBM
 };
 
-// Samples whose weights are held at once, and shares of the support vectors in the second product: about
-// 2,048 workgroups of it (two rounds of what the device holds), 16 shares at most.
+// Short rows (up to 128 features) are taken in one kernel, the others in two products.
+constexpr int64_t SHORT_D = 128;
+constexpr int short_q(int fb) { return fb <= 4 ? 4 : 2; }  // blocks of 16 samples a wave holds
+
+// Samples whose weights are held at once, and shares of the support vectors: about 2,048 workgroups (two rounds
+// of what the device holds), 16 shares at most (short rows: 32).
 GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
   GradTiles t{};
   t.svp = round_up(n, ST);
   t.dc = round_up(d, 4);
+  t.nblocks = (int32_t)(div_up(n, 1024) > COMPACT_MAX ? COMPACT_MAX : div_up(n, 1024));
+  if (d <= SHORT_D) {
+    t.fb = (int32_t)div_up(d, 16);
+    const int64_t qt = 64 * short_q(t.fb), s = 2048 / div_up(m, qt);
+    t.mc = round_up(m, qt);
+    t.splits = (int32_t)(s < 1 ? 1 : s > 32 ? 32 : s);
+    return t;
+  }
   const int64_t most = WEIGHT_BYTES / (4 * t.svp) / ST * ST;
   t.mc = round_up(m, ST);
   if (t.mc > most) t.mc = most < ST ? ST : most;
   const int64_t tiles = t.mc / ST * div_up(d, ST), s = 2048 / tiles;
   t.splits = (int32_t)(s < 1 ? 1 : s > 16 ? 16 : s);
-  t.nblocks = (int32_t)(div_up(n, 1024) > COMPACT_MAX ? COMPACT_MAX : div_up(n, 1024));
   return t;
 }
+
+// Bytes of one block of 32 support vectors of `fb` blocks of features (grad_pack_k).
+__host__ __device__ constexpr int64_t image_bytes(int fb) { return 1024 * (4 * ((fb + 1) / 2) + 2 * fb + 1); }
 
 // Places everything in ws (NULL: only counts); returns the bytes.
 int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool objective) {
@@ -246,35 +263,40 @@ int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool
   t.cmax = static_cast<float *>(take(4 * COMPACT_MAX));
   t.sv = split_views(take(gram_split_scratch_bytes(n, d)), n, d);
   t.q = objective ? t.sv : split_views(take(gram_split_scratch_bytes(m, d)), m, d);
-  t.xt.dp = t.p.dp = t.svp;
-  t.xt.rows = static_cast<_Float16 *>(take(4 * d * t.svp));
-  t.p.rows = static_cast<_Float16 *>(take(4 * t.mc * t.svp));
-  t.sums = static_cast<float *>(take(4 * t.svp / 64 * t.mc));
+  if (t.fb) {
+    t.image = static_cast<char *>(take(t.svp / 32 * image_bytes(t.fb)));
+    t.sums = static_cast<float *>(take(4 * t.splits * t.mc));
+  } else {
+    t.xt.dp = t.p.dp = t.svp;
+    t.xt.rows = static_cast<_Float16 *>(take(4 * d * t.svp));
+    t.p.rows = static_cast<_Float16 *>(take(4 * t.mc * t.svp));
+    t.sums = static_cast<float *>(take(4 * t.svp / 64 * t.mc));
+  }
   t.part = static_cast<float *>(take(4 * t.splits * t.mc * t.dc));
   return (int64_t)(at - base) + 256;
 }
 
 // Support vectors in index order (every workgroup counts those before its share itself), their c_j, and the
 // largest |c_j| of the share.
-__global__ void __launch_bounds__(TB) grad_compact_k(SvGradCall c, GradTiles t) {
-  __shared__ int red[TB / 64];
-  __shared__ float top[TB / 64];
+__global__ void __launch_bounds__(CB) grad_compact_k(SvGradCall c, GradTiles t) {
+  __shared__ int red[CB / 64];
+  __shared__ float top[CB / 64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t chunk = ((c.n + gridDim.x - 1) / gridDim.x + TB - 1) / TB * TB;
+  const int64_t chunk = ((c.n + gridDim.x - 1) / gridDim.x + CB - 1) / CB * CB;
   const int64_t c0 = min(c.n, blockIdx.x * chunk), c1 = min(c.n, c0 + chunk);
   int before = 0;
 #pragma unroll 16
-  for (int64_t j = threadIdx.x; j < c0; j += TB) before += c.alpha[j] > 0.0 ? 1 : 0;
+  for (int64_t j = threadIdx.x; j < c0; j += CB) before += c.alpha[j] > 0.0 ? 1 : 0;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
   if (lane == 0) red[w] = before;
   __syncthreads();
   int base = 0;
 #pragma unroll
-  for (int q = 0; q < TB / 64; ++q) base += red[q];
+  for (int q = 0; q < CB / 64; ++q) base += red[q];
   __syncthreads();
   float most = 0.f;
-  for (int64_t j0 = c0; j0 < c1; j0 += TB) {
+  for (int64_t j0 = c0; j0 < c1; j0 += CB) {
     const int64_t j = j0 + threadIdx.x;
     const double a = j < c1 ? c.alpha[j] : 0.0;
     const unsigned long long mask = __ballot(a > 0.0);
@@ -282,7 +304,7 @@ __global__ void __launch_bounds__(TB) grad_compact_k(SvGradCall c, GradTiles t) 
     __syncthreads();
     int off = __popcll(mask & ((1ull << lane) - 1ull)), tot = 0;
 #pragma unroll
-    for (int q = 0; q < TB / 64; ++q) {
+    for (int q = 0; q < CB / 64; ++q) {
       off += q < w ? red[q] : 0;
       tot += red[q];
     }
@@ -300,7 +322,9 @@ __global__ void __launch_bounds__(TB) grad_compact_k(SvGradCall c, GradTiles t) 
   if (lane == 0) top[w] = most;
   __syncthreads();
   if (threadIdx.x != 0) return;
-  t.cmax[blockIdx.x] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+#pragma unroll
+  for (int q = 1; q < CB / 64; ++q) most = fmaxf(most, top[q]);
+  t.cmax[blockIdx.x] = most;
   if (blockIdx.x == gridDim.x - 1) t.count[0] = base;
   if (blockIdx.x == 0) t.count[1] = 0;
 }
@@ -380,6 +404,14 @@ __device__ __forceinline__ bool xcd_item(int64_t tiles, int64_t i, int64_t &item
 
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
+// p as a rounded fp32, once and for all.  A product that is converted to fp16 may be fused with the conversion, which
+// then rounds once, while its other uses round twice: a value near a tie gave a high half one step from the
+// one its low half had been taken from.
+__device__ __forceinline__ float rounded(float p) {
+  asm("" : "+v"(p));
+  return p;
+}
+
 // Weights of 128 samples x 128 support vectors.  The support vectors are the MFMA's row operand, so a lane
 // holds 4 consecutive ones of a sample and stores 8 bytes of each half.  Tiles in the order (8 tiles of
 // samples) x support vectors.
@@ -440,7 +472,7 @@ __global__ void __launch_bounds__(SBS, 3) grad_weights_k(SvGradCall c, GradTiles
         float p = ca[e] * __builtin_amdgcn_exp2f(cexp * d2);
         if (objective && s0 + lr + e == q0 + lc) p = 0.f;
         sum[b] += p;
-        p *= sa[e] * norm;
+        p = rounded(p * (sa[e] * norm));
         h[e] = (_Float16)p;
         l[e] = (_Float16)(p - (float)h[e]);
       }
@@ -510,6 +542,209 @@ __global__ void __launch_bounds__(SBS, 4) grad_product_k(SvGradCall c, GradTiles
   } while (st < st1);
 }
 
+// ---------------------------------------------------------------------------- short rows
+//
+// Up to 128 features both products fit one kernel, and the weights never leave the registers: a wave holds 16 QB
+// samples (their split rows and the sums of all features) and walks blocks of 32 support vectors.  In the first
+// product the support vectors are the row operand, so a lane ends up with the weights of sample l % 16
+// and support vectors 4 (l / 16) + e and 16 + 4 (l / 16) + e: eight values that are an operand of the second
+// product as they stand, if the other operand lists its support vectors in that order.
+// grad_pack_k lays a block out as it is to stand in LDS, so a stage is a straight copy:
+//   [feature chunk of 32][support vector][hi 32 | lo 32]   the rows, 16-byte pieces permuted by ^ (row % 8)
+//   [feature][hi 32 | lo 32]                               the same by feature, pieces permuted likewise
+//   [3][32] floats: row scale, -gamma log2(e) |x|^2, c_j 2^W_EXP / 2^ec
+__device__ __forceinline__ int sv_slot(int j) {  // support vector at place j of an operand
+  return (j & 4) ? 16 + 4 * (j >> 3) + (j & 3) : 4 * (j >> 3) + (j & 3);
+}
+
+__global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, float cexp) {
+  const int nsv = t.count[0], s0 = blockIdx.x * 32, nk = (t.fb + 1) / 2;
+  if (s0 >= nsv) return;
+  char *img = t.image + blockIdx.x * image_bytes(t.fb);
+  const int ec = coef_exp(t);
+  int es = 0;
+  (void)frexpf(__int_as_float(t.count[1]), &es);
+  for (int p = threadIdx.x; p < nk * 256; p += TB) {  // a piece of the rows
+    const int k = p >> 8, row = (p >> 3) & 31, piece = (p & 7) ^ (row & 7);
+    split_h8 v = {};
+    if (s0 + row < nsv)
+      v = *reinterpret_cast<const split_h8 *>(t.sv.rows + (int64_t)(s0 + row) * 2 * t.sv.dp + k * 64 + piece * 8);
+    *reinterpret_cast<split_h8 *>(img + 16 * p) = v;
+  }
+  img += nk * 4096;
+  // a piece by feature, hi and lo: features by threads, so that rows are read along them
+  for (int p = threadIdx.x; p < t.fb * 16 * 4; p += TB) {
+    const int f = p % (t.fb * 16), g = p / (t.fb * 16);
+    split_h8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = s0 + sv_slot(8 * g + e);
+      float x = 0.f;
+      if (j < nsv && f < c.d && t.sv.nrm[j] < INFINITY) x = ldexpf(c.X[(int64_t)t.sv_row[j] * c.d + f], X_EXP - es);
+      h[e] = (_Float16)x;
+      l[e] = (_Float16)(x - (float)h[e]);
+    }
+    *reinterpret_cast<split_h8 *>(img + f * 128 + ((g ^ (f & 7)) << 4)) = h;
+    *reinterpret_cast<split_h8 *>(img + f * 128 + (((g | 4) ^ (f & 7)) << 4)) = l;
+  }
+  img += t.fb * 2048;
+  if (threadIdx.x < 32) {
+    const int j = s0 + threadIdx.x;
+    const bool in = j < nsv && t.sv.nrm[j] < INFINITY;  // (an infinite norm: only copies of the row are near it)
+    float *o = reinterpret_cast<float *>(img) + threadIdx.x;
+    o[0] = in ? t.sv.scale[j] : 0.f;
+    o[32] = in ? cexp * t.sv.nrm[j] : 0.f;
+    o[64] = in ? ldexpf(t.coef[j], W_EXP - ec) : 0.f;
+  }
+}
+
+template <int FB>
+__global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c, GradTiles t, float cexp) {
+  constexpr int NK = (FB + 1) / 2, QB = short_q(FB), CHUNKS = (int)(image_bytes(FB) / 1024);
+  __shared__ __align__(16) char lds[2][image_bytes(FB)];
+  const bool objective = c.Q == nullptr;
+  const int nsv = t.count[0];
+  const int64_t q_end = objective ? nsv : c.m;
+  const int64_t q0 = (int64_t)blockIdx.x * 64 * QB;
+  if (q0 >= q_end || nsv == 0) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, r16 = lane & 15, split = blockIdx.y;
+  const int stages = (nsv + 31) / 32, per = (stages + t.splits - 1) / t.splits;
+  const int st0 = min(stages, split * per), st1 = min(stages, st0 + per);
+  const int64_t qw = q0 + w * 16 * QB;  // this wave's samples
+  h8 qh[QB][NK], ql[QB][NK];
+  float sb[QB], nb[QB], sum[QB];
+  v4f acc[QB][FB];
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    const int64_t q = min(qw + b * 16 + r16, q_end - 1);
+    const _Float16 *row = t.q.rows + q * 2 * t.q.dp;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      qh[b][k] = *reinterpret_cast<const h8 *>(row + k * 64 + g * 8);
+      ql[b][k] = *reinterpret_cast<const h8 *>(row + k * 64 + 32 + g * 8);
+    }
+    const float n = t.q.nrm[q];
+    sb[b] = n < INFINITY ? -2.0f * cexp * t.q.scale[q] : 0.f;
+    nb[b] = cexp * n;
+    sum[b] = 0.f;
+#pragma unroll
+    for (int f = 0; f < FB; ++f) acc[b][f] = (v4f){0.f, 0.f, 0.f, 0.f};
+  }
+  const auto fetch = [&](int st, int buf) {
+    const char *src = t.image + (int64_t)st * image_bytes(FB) + lane * 16;
+#pragma unroll
+    for (int ch = 0; ch < (CHUNKS + 3) / 4; ++ch)
+      if (ch * 4 + w < CHUNKS)
+        __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)(src + (ch * 4 + w) * 1024),
+                                         (__attribute__((address_space(3))) void *)&lds[buf][(ch * 4 + w) * 1024], 16, 0, 0);
+  };
+  const auto leave = [&](bool again) {  // the sums so far to this share's place
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+      float s = sum[b];
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      const int64_t l = (int64_t)split * t.mc + qw + b * 16 + r16;
+      if (g == 0) t.sums[l] = again ? t.sums[l] + s : s;
+      sum[b] = 0.f;
+#pragma unroll
+      for (int f = 0; f < FB; ++f) {
+        if (f * 16 + 4 * g < t.dc) {
+          v4f *o = reinterpret_cast<v4f *>(&t.part[l * t.dc + f * 16 + 4 * g]);
+          if (again) acc[b][f] += *o;
+          *o = acc[b][f];
+        }
+        acc[b][f] = (v4f){0.f, 0.f, 0.f, 0.f};
+      }
+    }
+  };
+  if (st0 < st1) fetch(st0, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  int buf = 0;
+  for (int st = st0; st < st1; ++st) {
+    if (st + 1 < st1) fetch(st + 1, buf ^ 1);
+    const h8 *rows = reinterpret_cast<const h8 *>(lds[buf]);
+    const h8 *feat = reinterpret_cast<const h8 *>(lds[buf] + NK * 4096);
+    const float *sc = reinterpret_cast<const float *>(lds[buf] + NK * 4096 + FB * 2048);
+    v4f s[QB][2];
+#pragma unroll
+    for (int b = 0; b < QB; ++b)
+#pragma unroll
+      for (int v = 0; v < 2; ++v) s[b][v] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const int row = v * 16 + r16;
+        const h8 xh = rows[k * 256 + row * 8 + (g ^ (r16 & 7))], xl = rows[k * 256 + row * 8 + ((g | 4) ^ (r16 & 7))];
+#pragma unroll
+        for (int b = 0; b < QB; ++b) s[b][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, qh[b][k], s[b][v], 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) s[b][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, ql[b][k], s[b][v], 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) s[b][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, qh[b][k], s[b][v], 0, 0, 0);
+      }
+    }
+    h8 ph[QB], pl[QB];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const v4f sa = *reinterpret_cast<const v4f *>(&sc[v * 16 + 4 * g]);
+      const v4f na = *reinterpret_cast<const v4f *>(&sc[32 + v * 16 + 4 * g]);
+      const v4f ca = *reinterpret_cast<const v4f *>(&sc[64 + v * 16 + 4 * g]);
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float u = __builtin_fmaf(s[b][v][e], sa[e] * sb[b], na[e] + nb[b]);  // -gamma log2(e) |x_j - x_q|^2
+          u = u < 0.f ? u : 0.f;
+          s[b][v][e] = rounded(ca[e] * __builtin_amdgcn_exp2f(u));
+        }
+      }
+    }
+    if (objective) {  // the pair of a sample with itself, in the blocks that hold both
+      const int64_t j0 = (int64_t)st * 32;
+      if (j0 < qw + 16 * QB && j0 + 32 > qw) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b)
+#pragma unroll
+          for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (j0 + v * 16 + 4 * g + e == qw + b * 16 + r16) s[b][v][e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b)
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = s[b][v][e];
+          sum[b] += p;
+          ph[b][4 * v + e] = (_Float16)p;
+          pl[b][4 * v + e] = (_Float16)(p - (float)ph[b][4 * v + e]);
+        }
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+      const int row = (f * 16 + r16) * 8;
+      const h8 xh = feat[row + (g ^ (r16 & 7))], xl = feat[row + ((g | 4) ^ (r16 & 7))];
+#pragma unroll
+      for (int b = 0; b < QB; ++b) acc[b][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, ph[b], acc[b][f], 0, 0, 0);
+#pragma unroll
+      for (int b = 0; b < QB; ++b) acc[b][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, pl[b], acc[b][f], 0, 0, 0);
+#pragma unroll
+      for (int b = 0; b < QB; ++b) acc[b][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, ph[b], acc[b][f], 0, 0, 0);
+    }
+    if ((st - st0) % FOLD == FOLD - 1 && st + 1 < st1) leave(st - st0 >= FOLD);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next block has landed
+    __syncthreads();                                  // and this one has been read
+    buf ^= 1;
+  }
+  leave(st1 - st0 > FOLD);
+}
+
 // One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x).
 __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
   const bool objective = c.Q == nullptr;
@@ -525,9 +760,10 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   const double f = nsv ? ldexp(2.0 * c.gamma * up, ec) : 0.0;
   const double scale = ldexp(1.0, es - W_EXP - X_EXP);
   float s = 0.f;
-  for (int64_t k = lane; k < (nsv + ST - 1) / ST * 2; k += 64) s += t.sums[k * t.mc + l];
+  for (int64_t k = lane; k < (t.fb ? t.splits : (nsv + ST - 1) / ST * 2); k += 64) s += nsv ? t.sums[k * t.mc + l] : 0.f;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (t.fb) s *= ldexpf(1.0f, -W_EXP);
   const float *x = (objective ? c.X : c.Q) + row * c.d;
   for (int64_t at = 4 * lane; at < c.d; at += 256) {
     float xv[4], o[4] = {};
@@ -555,15 +791,32 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   const bool objective = c.Q == nullptr;
   GradTiles t = tile_plan(c.n, c.d, c.m);
   tile_views(t, ws, c.n, c.d, c.m, objective);
-  hipLaunchKernelGGL(grad_compact_k, dim3((unsigned)t.nblocks), dim3(TB), 0, s, c, t);
+  hipLaunchKernelGGL(grad_compact_k, dim3((unsigned)t.nblocks), dim3(CB), 0, s, c, t);
   SplitRows sv = split_rows_of(c.X, c.n, t.sv), q = split_rows_of(objective ? c.X : c.Q, objective ? 0 : c.m, t.q);
   sv.perm = t.sv_row;
   const int64_t svb = split_rows_blocks(sv), qb = split_rows_blocks(q);
   hipLaunchKernelGGL(grad_split_k, dim3((unsigned)(svb + qb)), dim3(TB), 0, s, sv, q, c.d, t.count, (int32_t)svb);
+  const float cexp = (float)(-c.gamma * 1.4426950408889634);
+  if (objective) hipLaunchKernelGGL(grad_zero_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c);
+  if (t.fb) {
+    hipLaunchKernelGGL(grad_pack_k, dim3((unsigned)(t.svp / 32)), dim3(TB), 0, s, c, t, cexp);
+    const dim3 grid((unsigned)div_up(c.m, 64 * short_q(t.fb)), (unsigned)t.splits);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(TB), 0, s, c, t, cexp); };
+    switch (t.fb) {
+      case 1: go(grad_short_k<1>); break;
+      case 2: go(grad_short_k<2>); break;
+      case 3: go(grad_short_k<3>); break;
+      case 4: go(grad_short_k<4>); break;
+      case 5: go(grad_short_k<5>); break;
+      case 6: go(grad_short_k<6>); break;
+      case 7: go(grad_short_k<7>); break;
+      default: go(grad_short_k<8>);
+    }
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, (int64_t)0, c.m);
+    return hipGetLastError();
+  }
   if (div_up(c.d, 64) > 65535) return hipErrorInvalidValue;
   hipLaunchKernelGGL(grad_transpose_k, dim3((unsigned)(t.svp / 32), (unsigned)div_up(c.d, 64)), dim3(TB), 0, s, c.X, c.d, t);
-  if (objective) hipLaunchKernelGGL(grad_zero_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c);
-  const float cexp = (float)(-c.gamma * 1.4426950408889634);
   for (int64_t q0 = 0; q0 < c.m; q0 += t.mc) {
     const int64_t q1 = c.m - q0 < t.mc ? c.m : q0 + t.mc, nqt = div_up(q1 - q0, ST);
     const int64_t wb = round_up(nqt * (t.svp / ST), 8), pb = round_up(nqt * div_up(c.d, ST) * t.splits, 8);
