@@ -232,6 +232,7 @@ GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
   t.nblocks = (int32_t)(div_up(n, 1024) > COMPACT_MAX ? COMPACT_MAX : div_up(n, 1024));
   if (d <= SHORT_D) {
     t.fb = (int32_t)div_up(d, 16);
+    t.dc = round_up(d % 16 ? d + 1 : d, 4);
     const int64_t qt = 64 * short_q(t.fb), s = 2048 / div_up(m, qt);
     t.mc = round_up(m, qt);
     t.splits = (int32_t)(s < 1 ? 1 : s > 32 ? 32 : s);
@@ -552,7 +553,11 @@ __global__ void __launch_bounds__(SBS, 4) grad_product_k(SvGradCall c, GradTiles
 // grad_pack_k lays a block out as it is to stand in LDS, so a stage is a straight copy:
 //   [feature chunk of 32][support vector][hi 32 | lo 32]   the rows, 16-byte pieces permuted by ^ (row % 8)
 //   [feature][hi 32 | lo 32]                               the same by feature, pieces permuted likewise
-//   [3][32] floats: row scale, -gamma log2(e) |x|^2, c_j 2^W_EXP / 2^ec
+//   [2][32] floats: -gamma log2(e) |x|^2, c_j 2^W_EXP / 2^ec
+// All rows have one scale, 2^X_EXP over the largest row's, so that no factor is left for each pair: a value is within
+// 2^-39 of the largest of all before it is multiplied, 2^-24 of rows up to 2^15 times smaller.  Where the features
+// leave room in their last block of 16, one more "feature" of ones turns the sum of the weights into a
+// column of the second product.
 __device__ __forceinline__ int sv_slot(int j) {  // support vector at place j of an operand
   return (j & 4) ? 16 + 4 * (j >> 3) + (j & 3) : 4 * (j >> 3) + (j & 3);
 }
@@ -564,12 +569,21 @@ __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, flo
   const int ec = coef_exp(t);
   int es = 0;
   (void)frexpf(__int_as_float(t.count[1]), &es);
-  for (int p = threadIdx.x; p < nk * 256; p += TB) {  // a piece of the rows
-    const int k = p >> 8, row = (p >> 3) & 31, piece = (p & 7) ^ (row & 7);
-    split_h8 v = {};
-    if (s0 + row < nsv)
-      v = *reinterpret_cast<const split_h8 *>(t.sv.rows + (int64_t)(s0 + row) * 2 * t.sv.dp + k * 64 + piece * 8);
-    *reinterpret_cast<split_h8 *>(img + 16 * p) = v;
+  const float scale = ldexpf(1.0f, X_EXP - es);
+  for (int p = threadIdx.x; p < nk * 128; p += TB) {  // a piece of the rows, hi and lo
+    const int k = p >> 7, row = (p >> 2) & 31, g = p & 3, f0 = k * 32 + g * 8;
+    split_h8 h, l;
+    const bool in = s0 + row < nsv && t.sv.nrm[min(s0 + row, nsv - 1)] < INFINITY;
+    const float *x = c.X + (int64_t)(in ? t.sv_row[s0 + row] : 0) * c.d;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = in && f0 + e < c.d ? x[f0 + e] * scale : 0.f;
+      h[e] = (_Float16)v;
+      l[e] = (_Float16)(v - (float)h[e]);
+    }
+    char *o = img + k * 4096 + row * 128;
+    *reinterpret_cast<split_h8 *>(o + ((g ^ (row & 7)) << 4)) = h;
+    *reinterpret_cast<split_h8 *>(o + (((g | 4) ^ (row & 7)) << 4)) = l;
   }
   img += nk * 4096;
   // a piece by feature, hi and lo: features by threads, so that rows are read along them
@@ -579,8 +593,8 @@ __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, flo
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int j = s0 + sv_slot(8 * g + e);
-      float x = 0.f;
-      if (j < nsv && f < c.d && t.sv.nrm[j] < INFINITY) x = ldexpf(c.X[(int64_t)t.sv_row[j] * c.d + f], X_EXP - es);
+      float x = f == c.d ? (float)(1 << X_EXP) : 0.f;
+      if (j < nsv && f < c.d && t.sv.nrm[j] < INFINITY) x = c.X[(int64_t)t.sv_row[j] * c.d + f] * scale;
       h[e] = (_Float16)x;
       l[e] = (_Float16)(x - (float)h[e]);
     }
@@ -592,14 +606,28 @@ __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, flo
     const int j = s0 + threadIdx.x;
     const bool in = j < nsv && t.sv.nrm[j] < INFINITY;  // (an infinite norm: only copies of the row are near it)
     float *o = reinterpret_cast<float *>(img) + threadIdx.x;
-    o[0] = in ? t.sv.scale[j] : 0.f;
-    o[32] = in ? cexp * t.sv.nrm[j] : 0.f;
-    o[64] = in ? ldexpf(t.coef[j], W_EXP - ec) : 0.f;
+    o[0] = in ? cexp * t.sv.nrm[j] : 0.f;
+    o[32] = in ? ldexpf(t.coef[j], W_EXP - ec) : 0.f;
   }
 }
 
-template <int FB>
-__global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c, GradTiles t, float cexp) {
+typedef __fp16 hr2 __attribute__((ext_vector_type(2)));
+
+// p - h.x and p - h.y, the conversion of h included.
+__device__ __forceinline__ float minus_low(float p, hr2 h) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+  return r;
+}
+__device__ __forceinline__ float minus_high(float p, hr2 h) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+  return r;
+}
+
+// ONES: the weights' sums come from the feature of ones.
+template <int FB, bool ONES>
+__global__ void __launch_bounds__(TB, 2) grad_short_k(SvGradCall c, GradTiles t, float cexp) {
   constexpr int NK = (FB + 1) / 2, QB = short_q(FB), CHUNKS = (int)(image_bytes(FB) / 1024);
   __shared__ __align__(16) char lds[2][image_bytes(FB)];
   const bool objective = c.Q == nullptr;
@@ -612,6 +640,8 @@ __global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c
   const int stages = (nsv + 31) / 32, per = (stages + t.splits - 1) / t.splits;
   const int st0 = min(stages, split * per), st1 = min(stages, st0 + per);
   const int64_t qw = q0 + w * 16 * QB;  // this wave's samples
+  int es = 0;
+  (void)frexpf(__int_as_float(t.count[1]), &es);
   h8 qh[QB][NK], ql[QB][NK];
   float sb[QB], nb[QB], sum[QB];
   v4f acc[QB][FB];
@@ -625,7 +655,7 @@ __global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c
       ql[b][k] = *reinterpret_cast<const h8 *>(row + k * 64 + 32 + g * 8);
     }
     const float n = t.q.nrm[q];
-    sb[b] = n < INFINITY ? -2.0f * cexp * t.q.scale[q] : 0.f;
+    sb[b] = n < INFINITY ? -2.0f * cexp * ldexpf(t.q.scale[q], es - X_EXP) : 0.f;
     nb[b] = cexp * n;
     sum[b] = 0.f;
 #pragma unroll
@@ -642,12 +672,14 @@ __global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c
   const auto leave = [&](bool again) {  // the sums so far to this share's place
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-      float s = sum[b];
-      s += __shfl_xor(s, 16);
-      s += __shfl_xor(s, 32);
       const int64_t l = (int64_t)split * t.mc + qw + b * 16 + r16;
-      if (g == 0) t.sums[l] = again ? t.sums[l] + s : s;
-      sum[b] = 0.f;
+      if (!ONES) {
+        float s = sum[b];
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (g == 0) t.sums[l] = again ? t.sums[l] + s : s;
+        sum[b] = 0.f;
+      }
 #pragma unroll
       for (int f = 0; f < FB; ++f) {
         if (f * 16 + 4 * g < t.dc) {
@@ -690,18 +722,20 @@ __global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c
     h8 ph[QB], pl[QB];
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
-      const v4f sa = *reinterpret_cast<const v4f *>(&sc[v * 16 + 4 * g]);
-      const v4f na = *reinterpret_cast<const v4f *>(&sc[32 + v * 16 + 4 * g]);
-      const v4f ca = *reinterpret_cast<const v4f *>(&sc[64 + v * 16 + 4 * g]);
+      const v4f na = *reinterpret_cast<const v4f *>(&sc[v * 16 + 4 * g]);
+      const v4f ca = *reinterpret_cast<const v4f *>(&sc[32 + v * 16 + 4 * g]);
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float u = __builtin_fmaf(s[b][v][e], sa[e] * sb[b], na[e] + nb[b]);  // -gamma log2(e) |x_j - x_q|^2
-          u = u < 0.f ? u : 0.f;
-          s[b][v][e] = rounded(ca[e] * __builtin_amdgcn_exp2f(u));
+          const float u = __builtin_fmaf(s[b][v][e], sb[b], na[e] + nb[b]);  // -gamma log2(e) |x_j - x_q|^2
+          s[b][v][e] = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(u), 0.f, 1.f);
         }
       }
+#pragma unroll
+      for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[b][v][e] = rounded(ca[e] * s[b][v][e]);
     }
     if (objective) {  // the pair of a sample with itself, in the blocks that hold both
       const int64_t j0 = (int64_t)st * 32;
@@ -720,11 +754,15 @@ __global__ void __launch_bounds__(TB, FB <= 2 ? 3 : 2) grad_short_k(SvGradCall c
 #pragma unroll
       for (int v = 0; v < 2; ++v)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = s[b][v][e];
-          sum[b] += p;
-          ph[b][4 * v + e] = (_Float16)p;
-          pl[b][4 * v + e] = (_Float16)(p - (float)ph[b][4 * v + e]);
+        for (int e = 0; e < 4; e += 2) {
+          // the high half truncated: what is left is exact in fp32, and the low half rounds it
+          const float p0 = s[b][v][e], p1 = s[b][v][e + 1];
+          if (!ONES) sum[b] += p0 + p1;
+          const hr2 h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
+          ph[b][4 * v + e] = (_Float16)h[0];
+          ph[b][4 * v + e + 1] = (_Float16)h[1];
+          pl[b][4 * v + e] = (_Float16)minus_low(p0, h);
+          pl[b][4 * v + e + 1] = (_Float16)minus_high(p1, h);
         }
 #pragma unroll
     for (int f = 0; f < FB; ++f) {
@@ -760,10 +798,12 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   const double f = nsv ? ldexp(2.0 * c.gamma * up, ec) : 0.0;
   const double scale = ldexp(1.0, es - W_EXP - X_EXP);
   float s = 0.f;
-  for (int64_t k = lane; k < (t.fb ? t.splits : (nsv + ST - 1) / ST * 2); k += 64) s += nsv ? t.sums[k * t.mc + l] : 0.f;
+  const bool ones = t.fb && c.d % 16;
+  for (int64_t k = lane; nsv && k < (t.fb ? t.splits : (nsv + ST - 1) / ST * 2); k += 64)
+    s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (t.fb) s *= ldexpf(1.0f, -W_EXP);
+  if (t.fb) s *= ldexpf(1.0f, ones ? -W_EXP - X_EXP : -W_EXP);
   const float *x = (objective ? c.X : c.Q) + row * c.d;
   for (int64_t at = 4 * lane; at < c.d; at += 256) {
     float xv[4], o[4] = {};
@@ -801,16 +841,18 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   if (t.fb) {
     hipLaunchKernelGGL(grad_pack_k, dim3((unsigned)(t.svp / 32)), dim3(TB), 0, s, c, t, cexp);
     const dim3 grid((unsigned)div_up(c.m, 64 * short_q(t.fb)), (unsigned)t.splits);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(TB), 0, s, c, t, cexp); };
+    const auto go = [&](auto ones, auto sums) {
+      hipLaunchKernelGGL(c.d % 16 ? ones : sums, grid, dim3(TB), 0, s, c, t, cexp);
+    };
     switch (t.fb) {
-      case 1: go(grad_short_k<1>); break;
-      case 2: go(grad_short_k<2>); break;
-      case 3: go(grad_short_k<3>); break;
-      case 4: go(grad_short_k<4>); break;
-      case 5: go(grad_short_k<5>); break;
-      case 6: go(grad_short_k<6>); break;
-      case 7: go(grad_short_k<7>); break;
-      default: go(grad_short_k<8>);
+      case 1: go(grad_short_k<1, true>, grad_short_k<1, false>); break;
+      case 2: go(grad_short_k<2, true>, grad_short_k<2, false>); break;
+      case 3: go(grad_short_k<3, true>, grad_short_k<3, false>); break;
+      case 4: go(grad_short_k<4, true>, grad_short_k<4, false>); break;
+      case 5: go(grad_short_k<5, true>, grad_short_k<5, false>); break;
+      case 6: go(grad_short_k<6, true>, grad_short_k<6, false>); break;
+      case 7: go(grad_short_k<7, true>, grad_short_k<7, false>); break;
+      default: go(grad_short_k<8, true>, grad_short_k<8, false>);
     }
     hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, (int64_t)0, c.m);
     return hipGetLastError();
