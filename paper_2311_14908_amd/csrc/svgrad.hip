@@ -221,7 +221,7 @@ struct GradTiles {
 
 // Short rows (up to 128 features) are taken in one kernel, the others in two products.
 constexpr int64_t SHORT_D = 128;
-constexpr int short_q(int fb) { return fb <= 4 ? 4 : 2; }  // blocks of 16 samples a wave holds
+constexpr int short_q(int fb) { return fb <= 2 ? 4 : 2; }  // blocks of 16 samples a wave holds
 
 // Samples whose weights are held at once, and shares of the support vectors: about 2,048 workgroups (two rounds
 // of what the device holds), 16 shares at most (short rows: 32).
@@ -627,7 +627,7 @@ __device__ __forceinline__ float minus_high(float p, hr2 h) {
 
 // ONES: the weights' sums come from the feature of ones.
 template <int FB, bool ONES>
-__global__ void __launch_bounds__(TB, 2) grad_short_k(SvGradCall c, GradTiles t, float cexp) {
+__global__ void __launch_bounds__(TB, FB <= 4 ? 3 : 2) grad_short_k(SvGradCall c, GradTiles t, float cexp) {
   constexpr int NK = (FB + 1) / 2, QB = short_q(FB), CHUNKS = (int)(image_bytes(FB) / 1024);
   __shared__ __align__(16) char lds[2][image_bytes(FB)];
   const bool objective = c.Q == nullptr;
