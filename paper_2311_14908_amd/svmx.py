@@ -404,14 +404,17 @@ _STATES = {torch.float32: SVM_F32, torch.float8_e4m3fn: SVM_F8}
 _tls = threading.local()
 
 
-def _stream_options():
-    """This thread's options with nothing set but the current stream."""
-    o = getattr(_tls, "options", None)
-    if o is None:
-        o = _tls.options = svm_options()
+def _stream_options(device: int):
+    """This thread's options with nothing set but the current stream of the device."""
+    try:
+        o, ref = _tls.options
+    except AttributeError:
+        o = svm_options()
         load().svm_default_options(C.byref(o))
-    o.stream = torch.cuda.current_stream().cuda_stream
-    return C.byref(o)
+        ref = C.byref(o)
+        _tls.options = o, ref
+    o.stream = torch._C._cuda_getCurrentRawStream(device)  # the handle alone, without a Stream object around it
+    return ref
 
 
 def _tensors(args):
@@ -438,21 +441,34 @@ def _streamed(f):
 
 
 def _on_device(t, name):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == torch.cuda.current_device()):
+    """The current device, which t must be on (get_device() of a host tensor is -1)."""
+    device = torch.cuda.current_device()
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
         raise TypeError(f"{name} must be a tensor on the current device")
+    return device
 
 
 def _float_rows(t, name, shape=None):
     """Type and pitch of a matrix of floats whose rows are contiguous."""
     _on_device(t, name)
-    if t.dtype not in _FLOATS:
+    kind = _FLOATS.get(t.dtype)
+    if kind is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
     if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
         raise ValueError(f"{name} must be a matrix" + (f" of shape {shape}" if shape else "") + f" (got {tuple(t.shape)})")
     n, d = t.shape
-    if (d > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < d):
+    ld, step = t.stride()
+    if (d > 1 and step != 1) or (n > 1 and ld < d):
         raise ValueError(f"{name} must have contiguous rows that do not overlap (strides {t.stride()})")
-    return _FLOATS[t.dtype], t.stride(0) if n > 1 else max(d, 1)
+    return kind, ld if n > 1 else max(d, 1)
+
+
+def _new_rows(n, d, dtype, like):
+    """A new matrix and its type."""
+    kind = _FLOATS.get(dtype)
+    if kind is None:
+        raise TypeError(f"rows are float32, bfloat16 or float16 (asked for {dtype})")
+    return torch.empty((n, d), dtype=dtype, device=like.device), kind
 
 
 def _vector(t, dtype, n, name):
@@ -463,26 +479,32 @@ def _vector(t, dtype, n, name):
 
 
 def _workspace(nbytes, device):
-    if nbytes < 0:
-        raise SvmError(SVM_EINVAL, "workspace size query failed")
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    """A tensor of nbytes and its address (None and 0 for none)."""
+    if nbytes <= 0:
+        if nbytes < 0:
+            raise SvmError(SVM_EINVAL, "workspace size query failed")
+        return None, None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr()
 
 
-def _token_args(tokens, bags, rows):
-    _on_device(tokens, "tokens")
+def _token_args(tokens, bags):
+    device = _on_device(tokens, "tokens")
     if tokens.dtype not in _TOKENS or tokens.dim() != 1 or not tokens.is_contiguous():
         raise TypeError("tokens must be a contiguous int32 or int64 vector")
     T = tokens.shape[0]
     if bags is None:
-        return T, T, None
+        return T, T, None, device
     _on_device(bags, "bags")
-    if bags.dim() != 1 or bags.shape[0] < 1 or (rows is not None and bags.shape[0] != rows + 1):
+    if bags.dtype != torch.int64 or bags.dim() != 1 or not bags.is_contiguous():
+        raise TypeError("bags must be a contiguous int64 vector")
+    if bags.shape[0] < 1:
         raise ValueError("bags must hold the start of every bag and the end of the last")
-    return T, bags.shape[0] - 1, _vector(bags, torch.int64, bags.shape[0], "bags")
+    return T, bags.shape[0] - 1, bags.data_ptr(), device
 
 
 def _raise_invalid(invalid):
-    if invalid is not None and int(invalid.item()):
+    if int(invalid.item()):
         raise SvmError(SVM_EINVAL, "a token outside the table, or bags that do not run from 0 to the number of tokens")
 
 
@@ -496,15 +518,16 @@ def svm_embed(table, tokens, *, bags=None, scale: float = 1.0, mean: bool = Fals
     lib = load()
     ttype, ld = _float_rows(table, "table")
     V, d = table.shape
-    T, B, bp = _token_args(tokens, bags, None)
-    out = torch.empty((B, d), dtype=out_dtype or table.dtype, device=table.device)
-    otype, ldo = _float_rows(out, "out")
-    ws = _workspace(lib.svm_embed_workspace_bytes(T, d, B, bp is not None), table.device)
+    T, B, bp, device = _token_args(tokens, bags)
+    out, otype = _new_rows(B, d, out_dtype or table.dtype, table)
+    nbytes = lib.svm_embed_workspace_bytes(T, d, B, bp is not None)
+    ws, wp = _workspace(nbytes, table.device)
     invalid = torch.zeros(1, dtype=torch.int32, device=table.device) if check else None
     _check(lib.svm_embed(table.data_ptr(), ttype, V, d, ld, tokens.data_ptr(), _TOKENS[tokens.dtype], T, bp, B, scale,
-                         int(mean), padding, out.data_ptr(), otype, ldo, _ptr(invalid), _ptr(ws),
-                         0 if ws is None else ws.shape[0], _stream_options()))
-    _raise_invalid(invalid)
+                         mean, padding, out.data_ptr(), otype, d, invalid.data_ptr() if check else None, wp, nbytes,
+                         _stream_options(device)))
+    if check:
+        _raise_invalid(invalid)
     return out
 
 
@@ -514,17 +537,23 @@ def svm_embed_grad(tokens, dY, V: int, *, bags=None, scale: float = 1.0, mean: b
     """Gradient of svm_embed in its table of V rows, given the rows' gradients dY.  ``out``: a table's gradient to
     add to (returned); else a new one of ``out_dtype`` (default: dY's)."""
     lib = load()
-    T, B, bp = _token_args(tokens, bags, None)
+    T, B, bp, device = _token_args(tokens, bags)
     ytype, ldy = _float_rows(dY, "dY", (B, dY.shape[-1]))
     d = dY.shape[1]
-    dE = torch.empty((V, d), dtype=out_dtype or dY.dtype, device=dY.device) if out is None else out
-    etype, lde = _float_rows(dE, "out", (V, d))
-    ws = _workspace(lib.svm_embed_grad_workspace_bytes(T, d, B), dY.device)
+    if out is None:
+        dE, etype = _new_rows(V, d, out_dtype or dY.dtype, dY)
+        lde = d
+    else:
+        dE = out
+        etype, lde = _float_rows(dE, "out", (V, d))
+    nbytes = lib.svm_embed_grad_workspace_bytes(T, d, B)
+    ws, wp = _workspace(nbytes, dY.device)
     invalid = torch.zeros(1, dtype=torch.int32, device=dY.device) if check else None
-    _check(lib.svm_embed_grad(tokens.data_ptr(), _TOKENS[tokens.dtype], T, bp, B, scale, int(mean), padding, dY.data_ptr(),
-                              ytype, ldy, dE.data_ptr(), etype, V, d, lde, int(out is not None), _ptr(invalid), _ptr(ws),
-                              ws.shape[0], _stream_options()))
-    _raise_invalid(invalid)
+    _check(lib.svm_embed_grad(tokens.data_ptr(), _TOKENS[tokens.dtype], T, bp, B, scale, mean, padding, dY.data_ptr(), ytype,
+                              ldy, dE.data_ptr(), etype, V, d, lde, out is not None, invalid.data_ptr() if check else None,
+                              wp, nbytes, _stream_options(device)))
+    if check:
+        _raise_invalid(invalid)
     return dE
 
 
@@ -547,12 +576,11 @@ def svm_layernorm(x, weight=None, bias=None, eps: float = 1e-5, *, out_dtype=Non
     xtype, ldx = _float_rows(x, "x")
     n, d = x.shape
     wp, bp, wdtype = _weight_args(x, weight, bias)
-    y = torch.empty((n, d), dtype=out_dtype or x.dtype, device=x.device)
-    ytype, ldy = _float_rows(y, "y")
-    stats = torch.empty((2, n), dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
-    _check(lib.svm_layernorm(x.data_ptr(), xtype, n, d, ldx, wp, bp, _FLOATS[wdtype], eps, y.data_ptr(), ytype, ldy,
-                             mean.data_ptr(), rstd.data_ptr(), _stream_options()))
+    y, ytype = _new_rows(n, d, out_dtype or x.dtype, x)
+    mean = torch.empty(n, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    _check(lib.svm_layernorm(x.data_ptr(), xtype, n, d, ldx, wp, bp, _FLOATS[wdtype], eps, y.data_ptr(), ytype, d,
+                             mean.data_ptr(), rstd.data_ptr(), _stream_options(x.get_device())))
     return y, mean, rstd
 
 
@@ -569,11 +597,12 @@ def svm_layernorm_grad(dy, x, mean, rstd, weight=None, *, weight_dtype=None):
         wdtype = weight_dtype
     dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
     dw, db = torch.empty(d, dtype=wdtype, device=x.device), torch.empty(d, dtype=wdtype, device=x.device)
-    ws = _workspace(lib.svm_layernorm_grad_workspace_bytes(n, d, xtype), x.device)
+    nbytes = lib.svm_layernorm_grad_workspace_bytes(n, d, xtype)
+    ws, wsp = _workspace(nbytes, x.device)
     _check(lib.svm_layernorm_grad(dy.data_ptr(), ytype, ldy, x.data_ptr(), xtype, n, d, ldx,
                                   _vector(mean, torch.float32, n, "mean"), _vector(rstd, torch.float32, n, "rstd"), wp,
-                                  _FLOATS[wdtype], dx.data_ptr(), d, dw.data_ptr(), db.data_ptr(), ws.data_ptr(),
-                                  ws.shape[0], _stream_options()))
+                                  _FLOATS[wdtype], dx.data_ptr(), d, dw.data_ptr(), db.data_ptr(), wsp, nbytes,
+                                  _stream_options(x.get_device())))
     return dx, dw, db
 
 
@@ -593,7 +622,7 @@ def svm_adamw_states(params, dtype=torch.float32):
 
 def _flat(t, types, count, device, name):
     """Address of a contiguous tensor of one of the types."""
-    if not t.is_cuda or t.get_device() != device:
+    if t.get_device() != device:
         raise TypeError(f"{name} must be on the current device")
     if t.dtype not in types or not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous and one of {[str(k) for k in types]} (got {t.dtype})")
@@ -614,44 +643,44 @@ def svm_adamw(params, grads, m, v, step: int, lr: float, *, beta1: float = 0.9, 
     on the gradients, a number or a one-element float32 device tensor (clipping by a norm known on the device)."""
     lib = load()
     count = len(params)
-    decay = [float(weight_decay)] * count if not isinstance(weight_decay, (list, tuple)) else weight_decay
+    decay = [weight_decay] * count if not isinstance(weight_decay, (list, tuple)) else weight_decay
     for name, lst in (("grads", grads), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale), ("master", master),
                       ("weight_decay", decay)):
         if lst is not None and len(lst) != count:
             raise ValueError(f"{name} must have one entry for each of the {count} params")
     device = torch.cuda.current_device()
-    words = np.zeros((max(count, 1), 11), dtype=np.int64)  # svm_adamw_tensor, 8 bytes a word
-    rows = []
-    for i in range(count):
-        p, g = params[i], grads[i]
+    tensors = (svm_adamw_tensor * count)()
+    for i, p in enumerate(params):
         n = p.numel()
-        f8 = m[i].dtype == torch.float8_e4m3fn
-        if f8 and (m_scale is None or v_scale is None):
-            raise ValueError("float8 states need m_scale and v_scale")
-        blocks = -(-n // ADAMW_BLOCK)
-        rows.append((_flat(p, _FLOATS, n, device, "params"),
-                     0 if master is None or master[i] is None else _flat(master[i], _F32_ONLY, n, device, "master"),
-                     _flat(g, _FLOATS, n, device, "grads"), _flat(m[i], _STATES, n, device, "m"),
-                     _flat(v[i], {m[i].dtype: 0}, n, device, "v"),
-                     _flat(m_scale[i], _F32_ONLY, blocks, device, "m_scale") if f8 else 0,
-                     _flat(v_scale[i], _F32_ONLY, blocks, device, "v_scale") if f8 else 0, n, 0,
-                     _FLOATS[p.dtype] | _FLOATS[g.dtype] << 32, SVM_F8 if f8 else SVM_F32))
-    if count:
-        words[:] = rows
-        words[:, 8] = np.asarray(decay, dtype=np.float64).view(np.int64)
+        t = tensors[i]
+        t.param = _flat(p, _FLOATS, n, device, "params")
+        t.grad = _flat(grads[i], _FLOATS, n, device, "grads")
+        t.m = _flat(m[i], _STATES, n, device, "m")
+        t.v = _flat(v[i], (m[i].dtype,), n, device, "v")
+        if m[i].dtype != torch.float32:
+            if m_scale is None or v_scale is None:
+                raise ValueError("float8 states need m_scale and v_scale")
+            blocks = -(-n // ADAMW_BLOCK)
+            t.m_scale = _flat(m_scale[i], _F32_ONLY, blocks, device, "m_scale")
+            t.v_scale = _flat(v_scale[i], _F32_ONLY, blocks, device, "v_scale")
+            t.state_type = SVM_F8
+        if master is not None and master[i] is not None:
+            t.master = _flat(master[i], _F32_ONLY, n, device, "master")
+        t.count, t.weight_decay, t.param_type, t.grad_type = n, decay[i], _FLOATS[p.dtype], _FLOATS[grads[i].dtype]
     a = svm_adamw_params(struct_size=C.sizeof(svm_adamw_params), step=step, lr=lr, beta1=beta1, beta2=beta2, eps=eps,
                          grad_scale=1.0)
     if isinstance(grad_scale, torch.Tensor):
         a.grad_scale_device = _flat(grad_scale, _F32_ONLY, 1, device, "grad_scale")
     else:
         a.grad_scale = grad_scale
-    _check(lib.svm_adamw(words.ctypes.data, count, C.byref(a), _stream_options()))
+    _check(lib.svm_adamw(tensors, count, C.byref(a), _stream_options(device)))
 
 
 def _machine_args(X, y, alpha):
     for t, dtype, name in ((X, torch.float32, "X"), (y, torch.int32, "y"), (alpha, torch.float64, "alpha")):
         _on_device(t, name)
-        _dev(t, dtype, name)
+        if t.dtype != dtype or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous {dtype} tensor")
     if X.dim() != 2 or y.shape != (X.shape[0],) or alpha.shape != (X.shape[0],):
         raise ValueError("X must be [n, d], y and alpha [n]")
     return X.shape
@@ -669,9 +698,10 @@ def svm_predict_grad(X_train, y, alpha, gamma: float, X_test, upstream=None) -> 
     m = X_test.shape[0]
     up = None if upstream is None else _vector(upstream, torch.float64, m, "upstream")
     dX = torch.empty((m, d), dtype=torch.float32, device=X_train.device)
-    ws = _workspace(lib.svm_predict_grad_workspace_bytes(n, d, m), X_train.device)
+    nbytes = lib.svm_predict_grad_workspace_bytes(n, d, m)
+    ws, wp = _workspace(nbytes, X_train.device)
     _check(lib.svm_predict_grad(X_train.data_ptr(), y.data_ptr(), alpha.data_ptr(), n, d, gamma, X_test.data_ptr(), m, up,
-                                dX.data_ptr(), _ptr(ws), 0 if ws is None else ws.shape[0], _stream_options()))
+                                dX.data_ptr(), wp, nbytes, _stream_options(X_train.get_device())))
     return dX
 
 
@@ -681,7 +711,8 @@ def svm_objective_grad(X, y, alpha, gamma: float) -> torch.Tensor:
     lib = load()
     n, d = _machine_args(X, y, alpha)
     dX = torch.empty((n, d), dtype=torch.float32, device=X.device)
-    ws = _workspace(lib.svm_objective_grad_workspace_bytes(n, d), X.device)
-    _check(lib.svm_objective_grad(X.data_ptr(), y.data_ptr(), alpha.data_ptr(), n, d, gamma, dX.data_ptr(), _ptr(ws),
-                                  0 if ws is None else ws.shape[0], _stream_options()))
+    nbytes = lib.svm_objective_grad_workspace_bytes(n, d)
+    ws, wp = _workspace(nbytes, X.device)
+    _check(lib.svm_objective_grad(X.data_ptr(), y.data_ptr(), alpha.data_ptr(), n, d, gamma, dX.data_ptr(), wp, nbytes,
+                                  _stream_options(X.get_device())))
     return dX
