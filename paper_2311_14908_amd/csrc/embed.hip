@@ -36,8 +36,12 @@ int64_t chunk_of(int64_t T, int64_t d) {
   return L;
 }
 
+// Token i.  Both widths are read as 32-bit words without a branch (a 64-bit token's second word, else the one word
+// again), so that the loads of several tokens are under way at once.
 __device__ __forceinline__ int64_t token_at(const EmbedCall &c, int64_t i) {
-  return c.wide ? static_cast<const int64_t *>(c.tokens)[i] : (int64_t)static_cast<const int32_t *>(c.tokens)[i];
+  const uint32_t *p = static_cast<const uint32_t *>(c.tokens);
+  const uint32_t lo = p[i << c.wide], hi = p[(i << c.wide) + c.wide];
+  return (int64_t)(((uint64_t)(c.wide ? hi : (uint32_t)((int32_t)lo >> 31)) << 32) | lo);
 }
 
 // First b in [0, count) with a[b] >= x, or count.
@@ -109,22 +113,24 @@ __device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &uni
 }
 
 // Sum of E[token] over positions lo .. hi - 1, EU rows on their way at once, the next EU tokens ahead of them;
-// `used` counts positions that are not padding.  A token outside the table reads nothing and makes the sum NaN.
+// `used` counts positions that are not padding, whose rows are added under a branch (all units of a chunk take
+// the same one), so nothing of a padding row gets in.  A token outside the table reads nothing and sets `bad`.
 template <int N, bool SMALL, class TE>
-__device__ __forceinline__ void sum_tokens(const EmbedCall &c, const TE *__restrict__ E, int64_t ld, int64_t lo, int64_t hi,
-                                           const Columns<N, SMALL> &col, float (&acc)[N], int &used) {
+__device__ __forceinline__ void sum_tokens(const EmbedCall &c, const TE *__restrict__ E, int64_t ld, int lo, int hi,
+                                           const Columns<N, SMALL> &col, float (&acc)[N], int &used, bool &bad) {
   if (lo >= hi) return;
   int64_t t[EU];
 #pragma unroll
   for (int q = 0; q < EU; ++q) t[q] = token_at(c, min(lo + q, hi - 1));
-  for (int64_t i = lo; i < hi; i += EU) {
+  for (int i = lo; i < hi; i += EU) {
     Raw<N, TE> v[EU];
-    bool live[EU], bad[EU];
+    bool live[EU];
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
       live[q] = i + q < hi && (c.padding < 0 || t[q] != c.padding);
-      bad[q] = live[q] && (t[q] < 0 || t[q] >= c.V);
-      v[q] = col.load(E + (live[q] && !bad[q] ? t[q] : 0) * ld);
+      const bool in = (uint64_t)t[q] < (uint64_t)c.V;
+      bad = bad || (live[q] && !in);
+      v[q] = col.load(E + (int64_t)(live[q] && in ? (uint32_t)t[q] : 0u) * ld);
     }
     if (i + EU < hi) {
 #pragma unroll
@@ -132,9 +138,10 @@ __device__ __forceinline__ void sum_tokens(const EmbedCall &c, const TE *__restr
     }
 #pragma unroll
     for (int q = 0; q < EU; ++q) {
-      used += live[q] ? 1 : 0;
+      if (!live[q]) continue;
+      ++used;
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += bad[q] ? __builtin_nanf("") : live[q] ? v[q].at(e) : 0.f;
+      for (int e = 0; e < N; ++e) acc[e] += v[q].at(e);
     }
   }
 }
@@ -191,7 +198,11 @@ __global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__rest
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
     int used = 0;
-    sum_tokens<N, SMALL>(c, E, ld, lo, hi, col, acc, used);
+    bool bad = false;
+    sum_tokens<N, SMALL>(c, E, ld, (int)lo, (int)hi, col, acc, used, bad);
+    if (bad)
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = __builtin_nanf("");
     const bool more = s1 > i1 && i1 < c.T;
     if (head || more) {
       const int64_t p = ch * 2 + (head ? 0 : 1);
@@ -299,7 +310,7 @@ __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32
 
 struct GradSpace {
   uint32_t *key[2], *src[2];  // [T]: token (V: none) and bag, before and after a pass of the sort
-  uint32_t *hist;             // [SORT_BLOCKS][2^DIGIT_MAX]
+  uint32_t *hist, *total;     // [SORT_BLOCKS][2^DIGIT_MAX], [2^DIGIT_MAX]
   int32_t *count;             // [B]: positions of a bag that count (mean)
   float *part;                // [chunks][2][d padded]
 };
@@ -317,6 +328,7 @@ GradSpace grad_views(void *ws, int64_t T, int64_t B) {
     g.src[k] = reinterpret_cast<uint32_t *>(take(4 * T));
   }
   g.hist = reinterpret_cast<uint32_t *>(take(4LL * SORT_BLOCKS << DIGIT_MAX));
+  g.total = reinterpret_cast<uint32_t *>(take(4LL << DIGIT_MAX));
   g.count = reinterpret_cast<int32_t *>(take(4 * B));
   g.part = reinterpret_cast<float *>(p);
   return g;
@@ -377,10 +389,16 @@ struct FillCall {
 };
 
 // Up to RANK_MAX positions: the place of a position is the number of positions with a smaller token, or the
-// same token and a smaller index.  16 positions a workgroup, and 16 threads a position that take every
-// 16th four of the others, so the LDS reads of a wave's four slices are one after the other in memory.
-// Blocks past the sort's zero dE meanwhile.
+// same token and a smaller index.  16 positions a workgroup, 16 lanes a position that take every 16th
+// four of the others (their LDS reads are one after the other in memory), and look for its bag among 16 starts
+// at a time.  Blocks past the sort's zero dE meanwhile.
 constexpr int RP = 16, RS = EB / RP;
+
+__device__ __forceinline__ int group_sum(int v) {
+#pragma unroll
+  for (int o = RS / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
 
 __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks) {
   if ((int64_t)blockIdx.x >= sort_blocks) {
@@ -388,57 +406,55 @@ __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, Fil
     return;
   }
   extern __shared__ uint32_t keys[];
-  __shared__ int ranks[RS][RP], counts[RS][RP];
-  const int T = (int)c.T, pos = threadIdx.x % RP, sl = threadIdx.x / RP;
+  const int T = (int)c.T, pos = threadIdx.x / RS, sl = threadIdx.x % RS;
   const int Tp = (T + 4 * RS - 1) / (4 * RS) * (4 * RS);
-  for (int j0 = threadIdx.x; j0 < Tp; j0 += 8 * EB) {
-    uint32_t k[8];
+  for (int j0 = threadIdx.x; j0 < Tp; j0 += 16 * EB) {
+    int64_t t[16];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {  // (V: padding; V + 1: outside the table)
+    for (int q = 0; q < 16; ++q) t[q] = token_at(c, min(j0 + q * EB, T - 1));
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {  // (V: padding; V + 1: outside the table)
       const int j = j0 + q * EB;
-      const int64_t t = token_at(c, min(j, T - 1));
-      k[q] = c.padding >= 0 && t == c.padding ? (uint32_t)c.V : t < 0 || t >= c.V ? (uint32_t)c.V + 1 : (uint32_t)t;
+      const uint32_t k = c.padding >= 0 && t[q] == c.padding ? (uint32_t)c.V
+                         : (uint64_t)t[q] >= (uint64_t)c.V   ? (uint32_t)c.V + 1
+                                                             : (uint32_t)t[q];
+      if (j < Tp) keys[j] = j < T ? k : 0xffffffffu;
     }
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (j0 + q * EB < Tp) keys[j0 + q * EB] = j0 + q * EB < T ? k[q] : 0xffffffffu;
   }
   const int p0 = blockIdx.x * RP, i = p0 + pos;
-  const int64_t b = bag_at(c, min(i, T - 1));
-  int64_t s0 = 0, s1 = 0;
-  if (c.mean && c.bags) {
+  int64_t b = i, s0 = 0, s1 = 0;
+  if (c.bags) {  // the last bag that starts at i or before: between lo and hi, a sixteenth of which is left each time
+    int64_t lo = 0, hi = c.B;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + RS - 1) / RS, at = lo + (sl + 1) * step;
+      const int below = group_sum(at < hi && c.bags[at] <= i ? 1 : 0);
+      lo += below * step;
+      hi = min(hi, lo + step);
+    }
+    b = lo;
     s0 = c.bags[b];
     s1 = min(c.bags[b + 1], c.T);
   }
   __syncthreads();
   const uint32_t k = i < T ? keys[i] : 0u;
   int rank = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int j = 4 * sl; j < Tp; j += 4 * RS) {
     const uint4 o = *reinterpret_cast<const uint4 *>(&keys[j]);
-    if (j + 4 <= p0) {
-      rank += (o.x <= k) + (o.y <= k) + (o.z <= k) + (o.w <= k);
-    } else if (j >= p0 + RP) {
-      rank += (o.x < k) + (o.y < k) + (o.z < k) + (o.w < k);
-    } else {
-      rank += (o.x < k || (o.x == k && j < i)) + (o.y < k || (o.y == k && j + 1 < i)) +
-              (o.z < k || (o.z == k && j + 2 < i)) + (o.w < k || (o.w == k && j + 3 < i));
-    }
+    // (o <= k) before the workgroup's positions, (o < k) after them, by index in between
+    const uint32_t before = j + 4 <= p0 ? k + 1 : k;
+    rank += (o.x < before) + (o.y < before) + (o.z < before) + (o.w < before);
+    if (j + 4 > p0 && j < p0 + RP)
+      rank += (o.x == k && j < i) + (o.y == k && j + 1 < i) + (o.z == k && j + 2 < i) + (o.w == k && j + 3 < i);
   }
-  ranks[sl][pos] = rank;
+  rank = group_sum(rank);
   // the first position of a bag counts the bag's that are not padding
   int used = 0;
-  if (i < T && i == s0)
+  if (c.mean && c.bags && i < T && i == s0) {
     for (int64_t j = s0 + sl; j < s1; j += RS) used += c.padding < 0 || keys[j] != (uint32_t)c.V ? 1 : 0;
-  counts[sl][pos] = used;
-  __syncthreads();
-  if (sl != 0 || i >= T) return;
-  rank = used = 0;
-#pragma unroll
-  for (int q = 0; q < RS; ++q) {
-    rank += ranks[q][pos];
-    used += counts[q][pos];
+    used = group_sum(used);
   }
+  if (sl != 0 || i >= T) return;
   g.key[0][rank] = min(k, (uint32_t)c.V);
   g.src[0][rank] = (uint32_t)b;
   if (c.mean && c.bags && i == s0) g.count[b] = used;
@@ -459,13 +475,22 @@ __global__ void __launch_bounds__(SB) embed_expand_k(EmbedCall c, GradSpace g, F
   h[threadIdx.x] = 0;
   __syncthreads();
   const int64_t i1 = min(c.T, (blockIdx.x + 1) * per);
-  for (int64_t i = blockIdx.x * per + threadIdx.x; i < i1; i += SB) {
-    const uint32_t k = key_at(c, i);
-    const int64_t b = bag_at(c, i);
-    g.key[0][i] = k;
-    g.src[0][i] = (uint32_t)b;
-    if (c.mean && c.bags) count_position(c, i, b, g.count);
-    atomicAdd(&h[k & mask], 1u);
+  for (int64_t j = blockIdx.x * per + threadIdx.x; j < i1; j += 4 * SB) {
+    uint32_t k[4];
+    int64_t b[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) k[q] = key_at(c, min(j + q * SB, i1 - 1));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) b[q] = bag_at(c, min(j + q * SB, i1 - 1));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = j + q * SB;
+      if (i >= i1) break;
+      g.key[0][i] = k[q];
+      g.src[0][i] = (uint32_t)b[q];
+      if (c.mean && c.bags) count_position(c, i, b[q], g.count);
+      atomicAdd(&h[k[q] & mask], 1u);
+    }
   }
   __syncthreads();
   g.hist[((int64_t)blockIdx.x << DIGIT_MAX) + threadIdx.x] = h[threadIdx.x];
@@ -483,26 +508,51 @@ __global__ void __launch_bounds__(SB) radix_count_k(const uint32_t *__restrict__
   hist[((int64_t)blockIdx.x << DIGIT_MAX) + threadIdx.x] = h[threadIdx.x];
 }
 
+// hist[block][digit] becomes the number of positions with this digit in blocks before, total[digit] that of all:
+// 64 digits a workgroup, 16 waves that each take a share of the blocks.
+constexpr int SC = 1024, SR = SORT_BLOCKS / (SC / 64);
+
+__global__ void __launch_bounds__(SC) radix_scan_k(uint32_t *__restrict__ hist, uint32_t *__restrict__ total, int blocks) {
+  __shared__ uint32_t sums[SC / 64][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t *h = hist + blockIdx.x * 64 + lane;
+  uint32_t v[SR], sum = 0;
+#pragma unroll
+  for (int q = 0; q < SR; ++q) v[q] = w * SR + q < blocks ? h[(w * SR + q) << DIGIT_MAX] : 0;
+#pragma unroll
+  for (int q = 0; q < SR; ++q) sum += v[q];
+  sums[w][lane] = sum;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int q = 0; q < SC / 64; ++q) {
+    before += q < w ? sums[q][lane] : 0;
+    all += sums[q][lane];
+  }
+#pragma unroll
+  for (int q = 0; q < SR; ++q) {
+    if (w * SR + q < blocks) h[(w * SR + q) << DIGIT_MAX] = before;
+    before += v[q];
+  }
+  if (w == 0) total[blockIdx.x * 64 + lane] = all;
+}
+
 // Every position of this block to its place: the positions with a smaller digit, those with its digit in
 // blocks before, and those before it in this block, 512 of them at a time (a wave counts its own by
 // ballots over the digit's bits).
 __global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__ key, const uint32_t *__restrict__ src,
                                                     uint32_t *__restrict__ key_out, uint32_t *__restrict__ src_out,
                                                     int64_t T, int shift, int bits, int64_t per,
-                                                    const uint32_t *__restrict__ hist) {
+                                                    const uint32_t *__restrict__ hist, const uint32_t *__restrict__ total) {
   __shared__ uint32_t base[SB];  // next place of each digit
   __shared__ uint32_t wave_n[SB / 64][SB];
   __shared__ uint32_t wsum[SB / 64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   const uint32_t dmask = (1u << bits) - 1u;
-  uint32_t before = 0, total = 0;
-#pragma unroll 32
-  for (int b = 0; b < (int)gridDim.x; ++b) {
-    const uint32_t v = hist[(b << DIGIT_MAX) + t];
-    before += b < (int)blockIdx.x ? v : 0;
-    total += v;
-  }
-  uint32_t incl = total;
+  const int64_t i0 = blockIdx.x * per, i1 = min(T, i0 + per);
+  uint32_t nk = i0 + t < i1 ? key[i0 + t] : 0, ns = i0 + t < i1 ? src[i0 + t] : 0;  // the next ones, on their way
+  const uint32_t all = t <= (int)dmask ? total[t] : 0, before = hist[((int64_t)blockIdx.x << DIGIT_MAX) + t];
+  uint32_t incl = all;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t v = __shfl_up(incl, o);
@@ -510,18 +560,18 @@ __global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__
   }
   if (lane == 63) wsum[w] = incl;
   __syncthreads();
-  uint32_t b0 = incl - total + before;
+  uint32_t b0 = incl - all + before;
   for (int q = 0; q < w; ++q) b0 += wsum[q];
   base[t] = b0;
 #pragma unroll
   for (int q = 0; q < SB / 64; ++q) wave_n[q][t] = 0;
   __syncthreads();
-  const int64_t i0 = blockIdx.x * per, i1 = min(T, i0 + per);
   for (int64_t r = i0; r < i1; r += SB) {
     const int64_t i = r + t;
     const bool in = i < i1;
-    const uint32_t k = in ? key[i] : 0, dig = (k >> shift) & dmask;
-    const uint32_t s = in ? src[i] : 0;
+    const uint32_t k = nk, s = ns, dig = (k >> shift) & dmask;
+    nk = i + SB < i1 ? key[i + SB] : 0;
+    ns = i + SB < i1 ? src[i + SB] : 0;
     unsigned long long same = __ballot(in);
 #pragma unroll
     for (int bit = 0; bit < DIGIT_MAX; ++bit) {
@@ -531,20 +581,25 @@ __global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__
     const uint32_t mine = __popcll(same & ((1ull << lane) - 1ull));
     if (in && mine == 0) wave_n[w][dig] = __popcll(same);
     __syncthreads();
-    if (in) {
-      uint32_t at = base[dig] + mine;
-      for (int q = 0; q < w; ++q) at += wave_n[q][dig];
-      key_out[at] = k;
-      src_out[at] = s;
-    }
-    __syncthreads();
-    uint32_t add = 0;
+    // the counts of the waves become the places where each of them starts; the thread of a digit sees to it
+    uint32_t at = base[t];
 #pragma unroll
     for (int q = 0; q < SB / 64; ++q) {
-      add += wave_n[q][t];
-      wave_n[q][t] = 0;
+      const uint32_t n = wave_n[q][t];
+      wave_n[q][t] = at;
+      at += n;
     }
-    base[t] += add;
+    base[t] = at;
+    __syncthreads();
+    uint32_t to = 0;
+    if (in) to = wave_n[w][dig] + mine;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < SB / 64; ++q) wave_n[q][t] = 0;
+    if (in) {
+      key_out[to] = k;
+      src_out[to] = s;
+    }
     __syncthreads();
   }
 }
@@ -634,9 +689,14 @@ __global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint3
     if (ch >= chunks || i1 >= c.T) return;
     run = key[i1];
     if (run >= (uint32_t)c.V || key[i1 - 1] != run || (i0 > 0 && key[i0 - 1] == run)) return;
-    // the first chunk whose end the run does not reach
-    int64_t last = ch + 1;
-    while (last - ch < SPAN && (last + 1) * L < c.T && key[(last + 1) * L - 1] == run && key[(last + 1) * L] == run) ++last;
+    int64_t last = ch + 1;  // the last chunk that starts inside the run (the keys are sorted: count them)
+    for (int64_t k = ch + 2; k <= ch + SPAN; k += 8) {
+      int more = 0;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) more += k + q <= ch + SPAN && key[min((k + q) * L, c.T - 1)] == run && (k + q) * L < c.T;
+      last += more;
+      if (more < 8) break;
+    }
     if (last - ch >= SPAN) return;
     join_short<N>(part, units, unit, ch, last, acc);
   } else {
@@ -747,7 +807,7 @@ hipError_t launch_embed(const EmbedCall &c, const void *table, int32_t table_typ
 }
 
 int64_t embed_grad_scratch_bytes(int64_t T, int64_t d, int64_t B) {
-  return 16 * T + (4LL * SORT_BLOCKS << DIGIT_MAX) + 4 * B + 4 * part_floats(T, d) + 8 * 256;
+  return 16 * T + (4LL * (SORT_BLOCKS + 1) << DIGIT_MAX) + 4 * B + 4 * part_floats(T, d) + 9 * 256;
 }
 
 hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type, int64_t ld_dy, void *de,
@@ -777,8 +837,9 @@ hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type
       const int shift = pass * bits;
       if (pass > 0)
         hipLaunchKernelGGL(radix_count_k, dim3((unsigned)nb), dim3(SB), 0, s, g.key[cur], c.T, shift, bits, per, g.hist);
+      hipLaunchKernelGGL(radix_scan_k, dim3((unsigned)div_up(1LL << bits, 64)), dim3(SC), 0, s, g.hist, g.total, (int)nb);
       hipLaunchKernelGGL(radix_place_k, dim3((unsigned)nb), dim3(SB), 0, s, g.key[cur], g.src[cur], g.key[1 - cur],
-                         g.src[1 - cur], c.T, shift, bits, per, g.hist);
+                         g.src[1 - cur], c.T, shift, bits, per, g.hist, g.total);
       cur = 1 - cur;
     }
   }
