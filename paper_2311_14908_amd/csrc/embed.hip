@@ -29,7 +29,9 @@ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Positions of a chunk: about 2^18 threads of 8 values each, between 16 positions (below, the joins cost
 // more than the rows) and 128 (above, nothing is gained).
+// Up to 64 positions are one chunk: a second launch costs more than they do.
 int64_t chunk_of(int64_t T, int64_t d) {
+  if (T <= 64) return 64;
   const double want = (double)T * (double)div_up(d, 8) / 131072.0;
   int64_t L = 16;
   while (L < 128 && (double)L < want) L <<= 1;
@@ -352,16 +354,16 @@ __device__ __forceinline__ void count_position(const EmbedCall &c, int64_t i, in
     if (i == c.bags[b]) count[b] = (int32_t)(c.bags[b + 1] - i);
     return;
   }
-  const bool live = token_at(c, i) != c.padding;
-  // the lanes of a wave that share the first lane's bag (all of them in a long bag) add up in one go
-  const int64_t first = ((int64_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
-                        (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
-  const unsigned long long same = __ballot(b == first && live);
-  if (b == first) {
-    if (live && (threadIdx.x & 63) == __builtin_ctzll(same)) atomicAdd(&count[b], __popcll(same));
-  } else if (live) {
-    atomicAdd(&count[b], 1);
-  }
+  // the lanes that share a bag are neighbours: the first of them adds for all
+  const int lane = threadIdx.x & 63;
+  const unsigned long long live = __ballot(token_at(c, i) != c.padding);
+  const int before = __shfl_up((int)b, 1);  // (bags are below 2^31)
+  const unsigned long long heads = __ballot(lane == 0 || before != (int)b);
+  if (!(heads >> lane & 1)) return;
+  const unsigned long long rest = lane == 63 ? 0 : heads >> (lane + 1);
+  const int width = rest ? __builtin_ctzll(rest) + 1 : 64 - lane;
+  const int n = __popcll(live >> lane & (width == 64 ? ~0ull : (1ull << width) - 1ull));
+  if (n) atomicAdd(&count[b], n);
 }
 
 // Zeros to this block's share of dE (blk of `blocks`), rows of `d` values ld apart.
@@ -460,6 +462,8 @@ __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, Fil
   if (c.mean && c.bags && i == s0) g.count[b] = used;
 }
 
+constexpr int STARTS = 2048;  // starts of bags a block of the sort holds
+
 // More positions: a stable radix sort, `bits` bits a pass (two passes up to 2^18 tokens).  Block b holds `per`
 // consecutive positions.  This kernel makes keys and bags and counts the first digit of every block; blocks
 // past the sort's zero dE.
@@ -470,18 +474,26 @@ __global__ void __launch_bounds__(SB) embed_expand_k(EmbedCall c, GradSpace g, F
     return;
   }
   __shared__ uint32_t h[1 << DIGIT_MAX];
+  __shared__ int64_t starts[STARTS];
   static_assert(SB == 1 << DIGIT_MAX, "a thread a digit");
   const uint32_t mask = (1u << bits) - 1u;
   h[threadIdx.x] = 0;
+  const int64_t i0 = blockIdx.x * per, i1 = min(c.T, i0 + per);
+  // the bags of this block's positions: their starts come into LDS where they fit
+  const int64_t b0 = bag_at(c, i0), nb = c.bags ? bag_at(c, i1 - 1) - b0 + 1 : 0;
+  const bool staged = nb > 0 && nb <= STARTS;
+  for (int64_t j = threadIdx.x; staged && j < nb; j += SB) starts[j] = c.bags[b0 + j];
   __syncthreads();
-  const int64_t i1 = min(c.T, (blockIdx.x + 1) * per);
-  for (int64_t j = blockIdx.x * per + threadIdx.x; j < i1; j += 4 * SB) {
+  for (int64_t j = i0 + threadIdx.x; j < i1; j += 4 * SB) {
     uint32_t k[4];
     int64_t b[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) k[q] = key_at(c, min(j + q * SB, i1 - 1));
 #pragma unroll
-    for (int q = 0; q < 4; ++q) b[q] = bag_at(c, min(j + q * SB, i1 - 1));
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = min(j + q * SB, i1 - 1);
+      b[q] = staged ? max<int64_t>(b0 + lower_bound<int64_t>(starts, nb, i + 1) - 1, b0) : bag_at(c, i);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t i = j + q * SB;
