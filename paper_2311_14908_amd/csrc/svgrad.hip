@@ -3,21 +3,22 @@
 // out_q = u_q 2 gamma sum_j c_j K(x_j, x_q) (x_j - x_q), c_j = a_j y_j.  The objective's gradient is the same
 // sum with the rows themselves as samples and u_q = -c_q (a_j y_j a_q y_q K is symmetric, which cancels the
 // 1/2), zero where a_q = 0; the pair j = q adds nothing and is left out.
-// Up to 16 samples of up to 1,024 features take a pass over the training rows.  More take two products in tiles of 128 x 128 on
-// the fp16 matrix cores with fp32 accuracy (split_tile.hpp), around a matrix of weights in HBM:
+// Up to 16 samples of up to 1,024 features take a pass over the training rows.  More take two products in tiles on
+// the fp16 matrix cores with fp32 accuracy (split_tile.hpp).  Rows of up to 128 features keep the kernel values
+// between them in registers (grad_short_k), longer ones in HBM:
 //   1. grad_compact_k: the support vectors in index order, their c_j, its largest magnitude;
 //   2. grad_split_k: split rows of the support vectors and of the samples;
-//      grad_transpose_k: the support vectors' rows once more, by feature, scaled by their row's 1 / s_j;
-//   3. grad_weights_k, for as many samples at a time as the workspace holds weights for: p_qj = c_j s_j K_qj,
-//      stored as two fp16 halves each, and sums of c_j K_qj over every 64 support vectors;
-//   4. grad_product_k: p times the rows by feature, over a share of the support vectors;
+//      grad_transpose_k: c_j x_j by feature, and c_j itself as one more feature;
+//   3. grad_kernel_k, for as many samples at a time as the workspace holds: K_qj as two fp16 halves;
+//   4. grad_product_k: K times the rows by feature, over shares of the support vectors;
 //   5. grad_finish_k: the shares' sums, minus (sum c_j K_qj) x_q, times u_q 2 gamma.
-// The weights are scaled to 2^15 and the rows to 2^14 at most before they are split: a half keeps 11 bits
-// only down to 2^-14, and a kernel value of 2^-25 still has all its 22 that way.
+// Kernel values are scaled to 2^15 and rows to 2^14 at most before they are split: a half keeps 11 bits only down
+// to 2^-14, and a kernel value of 2^-18 still has all its 22 that way.
 #include "layers.hpp"
 #include "rbf_d2.hpp"
 #include "split_rows.hpp"
 #include "split_tile.hpp"
+#include "tile_order.hpp"
 #include "units.hpp"
 
 namespace svmx {
@@ -197,38 +198,47 @@ constexpr int TB = 256;               // threads
 constexpr int CB = 1024;              // threads of the compaction
 constexpr int COMPACT_MAX = 64;       // and its workgroups
 constexpr int FOLD = 128;             // stages (of 32 support vectors) that one fp32 accumulator sums
-constexpr int W_EXP = 15, X_EXP = 14; // largest weight and row value, as powers of two
-constexpr int64_t WEIGHT_BYTES = 2LL << 30;  // weights held at once
+constexpr int W_EXP = 15, X_EXP = 14; // largest kernel value (short rows: weight) and row value, as powers of two
+constexpr int64_t KERNEL_BYTES = 2LL << 30;  // kernel values held at once
 
 inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 struct GradTiles {
   int32_t *sv_row;    // [n]
   float *coef;        // [n]: c_j (fp32)
-  int32_t *count;     // support vectors; [1]: bits of the largest row scale
+  int32_t *count;     // support vectors; [1]: bits of the largest row scale, [2]: exponent above every |c_j| x scale
   float *cmax;        // [COMPACT_MAX]: largest |c_j| of each workgroup of the compaction
   int32_t nblocks;    // of them
   SplitX sv, q;       // split rows (compact; q = sv for the objective's gradient)
-  SplitX xt;          // [d] rows by feature, dp = svp
-  SplitX p;           // [mc] rows of weights, dp = svp
-  float *sums;        // [svp / 64][mc]; short rows: [splits][mc]
+  SplitX xt;          // [d + 1] rows by feature, dp = svp
+  SplitX p;           // [mc] rows of kernel values, dp = svp
+  float *sums;        // short rows: [splits][mc]
   float *part;        // [splits][mc][dc]
   char *image;        // short rows: [svp / 32] blocks (grad_pack_k)
   int64_t mc, svp, dc;
   int32_t splits;
-  int32_t fb;         // short rows: blocks of 16 features; 0: two products around weights in HBM
+  int32_t fb;         // short rows: blocks of 16 features; 0: kernel values in HBM
+  int32_t fw;         // blocks of 16 features a wave of the second product holds
 };
 
 // Short rows (up to 128 features) are taken in one kernel, the others in two products.
 constexpr int64_t SHORT_D = 128;
 constexpr int short_q(int fb) { return fb <= 2 ? 4 : 2; }  // blocks of 16 samples a wave holds
 
-// Samples whose weights are held at once, and shares of the support vectors: about 2,048 workgroups (two rounds
-// of what the device holds), 16 shares at most (short rows: 32).
+// Features of a tile of the second product: 32 fw.  The count that leaves the fewest unused, of equals the largest
+// (fewer operand reads a product): 785 features are 5 tiles of 160 (15 unused), or 7 of 128 (111).
+int feature_blocks(int64_t features) {
+  int best = 5;
+  for (int f = 4; f >= 3; --f)
+    if (round_up(features, 32 * f) < round_up(features, 32 * best)) best = f;
+  return best;
+}
+
+// Samples whose kernel values are held at once, and shares of the support vectors (short rows: about 2,048
+// workgroups, 32 shares at most; else up to 8, chosen on the device, which knows the support vectors).
 GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
   GradTiles t{};
   t.svp = round_up(n, ST);
-  t.dc = round_up(d, 4);
   t.nblocks = (int32_t)(div_up(n, 1024) > COMPACT_MAX ? COMPACT_MAX : div_up(n, 1024));
   if (d <= SHORT_D) {
     t.fb = (int32_t)div_up(d, 16);
@@ -238,11 +248,12 @@ GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
     t.splits = (int32_t)(s < 1 ? 1 : s > 32 ? 32 : s);
     return t;
   }
-  const int64_t most = WEIGHT_BYTES / (4 * t.svp) / ST * ST;
+  t.dc = round_up(d + 1, 4);
+  t.fw = feature_blocks(d + 1);
+  const int64_t most = KERNEL_BYTES / (4 * t.svp) / ST * ST;
   t.mc = round_up(m, ST);
   if (t.mc > most) t.mc = most < ST ? ST : most;
-  const int64_t tiles = t.mc / ST * div_up(d, ST), s = 2048 / tiles;
-  t.splits = (int32_t)(s < 1 ? 1 : s > 16 ? 16 : s);
+  t.splits = 8;
   return t;
 }
 
@@ -260,7 +271,7 @@ int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool
   };
   t.sv_row = static_cast<int32_t *>(take(4 * n));
   t.coef = static_cast<float *>(take(4 * n));
-  t.count = static_cast<int32_t *>(take(8));
+  t.count = static_cast<int32_t *>(take(12));
   t.cmax = static_cast<float *>(take(4 * COMPACT_MAX));
   t.sv = split_views(take(gram_split_scratch_bytes(n, d)), n, d);
   t.q = objective ? t.sv : split_views(take(gram_split_scratch_bytes(m, d)), m, d);
@@ -269,9 +280,8 @@ int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool
     t.sums = static_cast<float *>(take(4 * t.splits * t.mc));
   } else {
     t.xt.dp = t.p.dp = t.svp;
-    t.xt.rows = static_cast<_Float16 *>(take(4 * d * t.svp));
+    t.xt.rows = static_cast<_Float16 *>(take(4 * (d + 1) * t.svp));
     t.p.rows = static_cast<_Float16 *>(take(4 * t.mc * t.svp));
-    t.sums = static_cast<float *>(take(4 * t.svp / 64 * t.mc));
   }
   t.part = static_cast<float *>(take(4 * t.splits * t.mc * t.dc));
   return (int64_t)(at - base) + 256;
@@ -327,59 +337,40 @@ __global__ void __launch_bounds__(CB) grad_compact_k(SvGradCall c, GradTiles t) 
   for (int q = 1; q < CB / 64; ++q) most = fmaxf(most, top[q]);
   t.cmax[blockIdx.x] = most;
   if (blockIdx.x == gridDim.x - 1) t.count[0] = base;
-  if (blockIdx.x == 0) t.count[1] = 0;
+  if (blockIdx.x == 0) {
+    t.count[1] = 0;
+    t.count[2] = -100000;
+  }
 }
 
 // Split rows of the support vectors (blocks up to sv_blocks) and of the samples; the largest scale of the
-// former (a maximum, so its order does not matter).
-__global__ void __launch_bounds__(TB) grad_split_k(SplitRows sv, SplitRows q, int64_t d, int32_t *__restrict__ count,
-                                                   int32_t sv_blocks) {
+// former, and the exponent of the largest |c_j| times the scale (maxima, so their order does not matter).
+__global__ void __launch_bounds__(TB) grad_split_k(SplitRows sv, SplitRows q, int64_t d, GradTiles t, int32_t sv_blocks) {
   if ((int)blockIdx.x >= sv_blocks) {
     split_rows_block(q, d, blockIdx.x - sv_blocks, gridDim.x - sv_blocks, [](int64_t pos) { return pos; });
     return;
   }
-  const int64_t nsv = count[0];
+  const int64_t nsv = t.count[0];
   sv.count = nsv;
   split_rows_block(sv, d, blockIdx.x, sv_blocks, [](int64_t pos) { return pos; });
   // this workgroup's own rows again: their scales, just written by lane 0 of each row group
   const int per = TB / sv.gs, g = threadIdx.x & (sv.gs - 1), mine = threadIdx.x / sv.gs;
-  int most = 0;
+  int most[2] = {0, -100000};
   for (int64_t r = (int64_t)blockIdx.x * per + mine; g == 0 && r < nsv; r += (int64_t)sv_blocks * per)
-    most = max(most, sv.s.nrm[r] < INFINITY ? __float_as_int(sv.s.scale[r]) : 0);
+    if (sv.s.nrm[r] < INFINITY) {
+      int ec = 0, es = 0;
+      (void)frexpf(t.coef[r], &ec);
+      (void)frexpf(sv.s.scale[r], &es);
+      most[0] = max(most[0], __float_as_int(sv.s.scale[r]));
+      most[1] = max(most[1], ec + es);
+    }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
-  if ((threadIdx.x & 63) == 0 && most > __atomic_load_n(&count[1], __ATOMIC_RELAXED)) atomicMax(&count[1], most);
-}
-
-// Rows by feature: 32 support vectors x 64 features a workgroup, through LDS; past the last support vector zeros.
-__global__ void __launch_bounds__(TB) grad_transpose_k(const float *__restrict__ X, int64_t d, GradTiles t) {
-  __shared__ float v[32][65];
-  const int nsv = t.count[0];
-  const int s0 = blockIdx.x * 32;
-  if (s0 >= (nsv + ST - 1) / ST * ST) return;
-  const int64_t f0 = (int64_t)blockIdx.y * 64;
+  for (int k = 0; k < 2; ++k) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = threadIdx.x / 64 + 4 * k, f = threadIdx.x % 64;
-    float x = 0.f;
-    if (s0 + r < nsv && f0 + f < d)
-      x = X[(int64_t)t.sv_row[s0 + r] * d + f0 + f] * (1.0f / t.sv.scale[s0 + r]) * (float)(1 << X_EXP);
-    v[r][f] = x;
+    for (int o = 32; o > 0; o >>= 1) most[k] = max(most[k], __shfl_xor(most[k], o));
+    if ((threadIdx.x & 63) == 0 && most[k] > __atomic_load_n(&t.count[1 + k], __ATOMIC_RELAXED))
+      atomicMax(&t.count[1 + k], most[k]);
   }
-  __syncthreads();
-  // thread: 8 support vectors of one feature
-  const int f = threadIdx.x / 4, r0 = threadIdx.x % 4 * 8;
-  if (f0 + f >= d) return;
-  split_h8 h, l;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float x = v[r0 + e][f];
-    h[e] = (_Float16)x;
-    l[e] = (_Float16)(x - (float)h[e]);
-  }
-  _Float16 *o = t.xt.rows + (f0 + f) * 2 * t.svp + (int64_t)s0 * 2 + r0;
-  *reinterpret_cast<split_h8 *>(o) = h;
-  *reinterpret_cast<split_h8 *>(o + 32) = l;
 }
 
 __device__ __forceinline__ float wave_most(float v) {
@@ -403,6 +394,44 @@ __device__ __forceinline__ bool xcd_item(int64_t tiles, int64_t i, int64_t &item
   return i / 8 < share && item < tiles;
 }
 
+// Rows by feature, c_j x_j at 2^X_EXP over the largest of all, and after the last feature c_j at 2^X_EXP over the
+// largest: 32 support vectors x 64 features a workgroup, through LDS; past the last support vector zeros.
+__global__ void __launch_bounds__(TB) grad_transpose_k(const float *__restrict__ X, int64_t d, GradTiles t) {
+  __shared__ float v[32][65];
+  const int nsv = t.count[0];
+  const int s0 = blockIdx.x * 32;
+  if (s0 >= (nsv + ST - 1) / ST * ST) return;
+  const int64_t f0 = (int64_t)blockIdx.y * 64;
+  const int ec = coef_exp(t);
+  const int ex = t.count[2];
+  const double one = ldexp(1.0, X_EXP - ec), scale = ldexp(1.0, X_EXP - ex);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = threadIdx.x / 64 + 4 * k, f = threadIdx.x % 64;
+    float x = 0.f;
+    // (a row whose norm overflows has no neighbour but its copies, which add nothing)
+    if (s0 + r < nsv && f0 + f <= d && t.sv.nrm[s0 + r] < INFINITY) {
+      const double c = (double)t.coef[s0 + r];
+      x = (float)(f0 + f < d ? (double)X[(int64_t)t.sv_row[s0 + r] * d + f0 + f] * (c * scale) : c * one);
+    }
+    v[r][f] = x;
+  }
+  __syncthreads();
+  // thread: 8 support vectors of one feature
+  const int f = threadIdx.x / 4, r0 = threadIdx.x % 4 * 8;
+  if (f0 + f > d) return;
+  split_h8 h, l;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = v[r0 + e][f];
+    h[e] = (_Float16)x;
+    l[e] = (_Float16)(x - (float)h[e]);
+  }
+  _Float16 *o = t.xt.rows + (f0 + f) * 2 * t.svp + (int64_t)s0 * 2 + r0;
+  *reinterpret_cast<split_h8 *>(o) = h;
+  *reinterpret_cast<split_h8 *>(o + 32) = l;
+}
+
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 
 // p as a rounded fp32, once and for all.  A product that is converted to fp16 may be fused with the conversion, which
@@ -413,22 +442,64 @@ __device__ __forceinline__ float rounded(float p) {
   return p;
 }
 
-// Weights of 128 samples x 128 support vectors.  The support vectors are the MFMA's row operand, so a lane
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad_move(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+
+// A 4 x 4 square in the four lanes of a quad, a row a lane: transposed.
+__device__ __forceinline__ void quad_transpose(uint32_t (&v)[4]) {
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+#pragma unroll
+  for (int p = 0; p < 4; p += 2) {
+    const uint32_t t = quad_move<0xB1>(odd ? v[p] : v[p + 1]);  // quad_perm [1,0,3,2]
+    v[p] = odd ? t : v[p];
+    v[p + 1] = odd ? v[p + 1] : t;
+  }
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const uint32_t t = quad_move<0x4E>(high ? v[p] : v[p + 2]);  // quad_perm [2,3,0,1]
+    v[p] = high ? t : v[p];
+    v[p + 2] = high ? v[p + 2] : t;
+  }
+}
+
+// Four kernel values (high half | low half << 16) to row `row`, column `col` (a multiple of 4).
+__device__ __forceinline__ void put_halves(const SplitX &p, int64_t row, int64_t col, const uint32_t (&v)[4]) {
+  uint2 h, l;
+  h.x = __builtin_amdgcn_perm(v[1], v[0], 0x05040100);  // low halves of both words
+  h.y = __builtin_amdgcn_perm(v[3], v[2], 0x05040100);
+  l.x = __builtin_amdgcn_perm(v[1], v[0], 0x07060302);
+  l.y = __builtin_amdgcn_perm(v[3], v[2], 0x07060302);
+  _Float16 *o = p.rows + row * 2 * p.dp + (col >> 5) * 64 + (col & 31);
+  *reinterpret_cast<uint2 *>(o) = h;
+  *reinterpret_cast<uint2 *>(o + 32) = l;
+}
+
+// Kernel values of 128 samples x 128 support vectors.  The support vectors are the MFMA's row operand, so a lane
 // holds 4 consecutive ones of a sample and stores 8 bytes of each half.  Tiles in the order (8 tiles of
-// samples) x support vectors.
-__global__ void __launch_bounds__(SBS, 3) grad_weights_k(SvGradCall c, GradTiles t, float cexp, int64_t q_first, int64_t q_end) {
+// samples) x support vectors.  SYM (the objective's gradient, all of its samples at once): tiles on and above the
+// diagonal only, the others stored from them, after a quad of lanes has exchanged its 4 x 4 values.
+template <bool SYM>
+__global__ void __launch_bounds__(SBS, 3) grad_kernel_k(SvGradCall c, GradTiles t, float cexp, int64_t q_first, int64_t q_end) {
   __shared__ SplitStage S;
-  __shared__ float sA[ST], nA[ST], cA[ST], sB[ST], nB[ST];
+  __shared__ float sA[ST], nA[ST], sB[ST], nB[ST];
   const bool objective = c.Q == nullptr;
   const int nsv = t.count[0];
   if (objective) q_end = min(q_end, (int64_t)nsv);
   if (q_first >= q_end || nsv == 0) return;
   const int64_t nst = (nsv + ST - 1) / ST, nqt = (q_end - q_first + ST - 1) / ST;
-  int64_t item;
-  if (!xcd_item(nst * nqt, blockIdx.x, item)) return;
-  const int64_t sup = item / (8 * nst), rem = item - sup * 8 * nst, wide = min((int64_t)8, nqt - 8 * sup);
-  const int64_t s0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / wide)) * ST;
-  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(8 * sup + rem % wide)) * ST;  // among those held
+  int64_t item, ts, tq;
+  if (!xcd_item(SYM ? nst * (nst + 1) / 2 : nst * nqt, blockIdx.x, item)) return;
+  if (SYM) {
+    upper_tile_super(item, nst, ts, tq);
+  } else {
+    const int64_t sup = item / (8 * nst), rem = item - sup * 8 * nst, wide = min((int64_t)8, nqt - 8 * sup);
+    ts = rem / wide;
+    tq = 8 * sup + rem % wide;
+  }
+  const int64_t s0 = (int64_t)__builtin_amdgcn_readfirstlane((int)ts) * ST;
+  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)tq) * ST;  // among those held
   const int64_t q0 = q_first + l0;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
@@ -439,102 +510,141 @@ __global__ void __launch_bounds__(SBS, 3) grad_weights_k(SvGradCall c, GradTiles
     src[q] = w < 2 ? split_src(t.sv, min<int64_t>(s0 + i, nsv - 1)) : split_src(t.q, min<int64_t>(q0 + i, q_end - 1));
   }
   split_stage_load(S, src);
-  const int ec = coef_exp(t);
   if (threadIdx.x < ST) {
     const int64_t j = min<int64_t>(s0 + threadIdx.x, nsv - 1), q = min<int64_t>(q0 + threadIdx.x, q_end - 1);
     const float nj = t.sv.nrm[j], nq = t.q.nrm[q];
-    // a row whose norm overflows has no neighbour but its copies, which add nothing
     sA[threadIdx.x] = nj < INFINITY ? t.sv.scale[j] : 0.f;
-    nA[threadIdx.x] = nj;
-    cA[threadIdx.x] = s0 + threadIdx.x < nsv && nj < INFINITY ? ldexpf(t.coef[j], -ec) : 0.f;
-    sB[threadIdx.x] = nq < INFINITY ? -2.0f * t.q.scale[q] : 0.f;
-    nB[threadIdx.x] = nq;
+    nA[threadIdx.x] = cexp * nj;
+    sB[threadIdx.x] = nq < INFINITY ? -2.0f * cexp * t.q.scale[q] : 0.f;
+    nB[threadIdx.x] = cexp * nq;
   }
-  int es = 0;
-  (void)frexpf(__int_as_float(t.count[1]), &es);
-  const float norm = ldexpf(1.0f, W_EXP - es);  // s_j norm <= 2^W_EXP
   v4f acc[4][4];
   split_tile_loaded(S, src, t.sv.dp / SKS, wm, wn, acc);
-  float sum[4] = {};
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     const int lr = wm * 64 + a * 16 + 4 * kq;
     const v4f sa = *reinterpret_cast<const v4f *>(&sA[lr]), na = *reinterpret_cast<const v4f *>(&nA[lr]);
-    const v4f ca = *reinterpret_cast<const v4f *>(&cA[lr]);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       const int lc = wn * 64 + b * 16 + r16;
       const float sb = sB[lc], nb = nB[lc];
-      h4 h, l;
+      uint32_t v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float d2 = __builtin_fmaf(acc[a][b][e] * sa[e], sb, na[e] + nb);
-        d2 = d2 > 0.f ? d2 : 0.f;
-        float p = ca[e] * __builtin_amdgcn_exp2f(cexp * d2);
-        if (objective && s0 + lr + e == q0 + lc) p = 0.f;
-        sum[b] += p;
-        p = rounded(p * (sa[e] * norm));
-        h[e] = (_Float16)p;
-        l[e] = (_Float16)(p - (float)h[e]);
+        const float u = __builtin_fmaf(acc[a][b][e], sa[e] * sb, na[e] + nb);  // -gamma log2(e) |x_j - x_q|^2
+        float k = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(u), 0.f, 1.f) * (float)(1 << W_EXP);
+        if (objective && s0 + lr + e == q0 + lc) k = 0.f;
+        k = rounded(k);
+        const _Float16 h = (_Float16)k, l = (_Float16)(k - (float)h);
+        v[e] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
       }
-      _Float16 *o = t.p.rows + (l0 + lc) * 2 * t.svp + ((s0 + lr) >> 5) * 64 + (lr & 31);
-      *reinterpret_cast<h4 *>(o) = h;
-      *reinterpret_cast<h4 *>(o + 32) = l;
+      put_halves(t.p, l0 + lc, s0 + lr, v);
+      if (SYM && s0 != q0) {
+        quad_transpose(v);
+        put_halves(t.p, s0 + lr + (r16 & 3), q0 + wn * 64 + b * 16 + (r16 & 12), v);
+      }
     }
-  }
-#pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    sum[b] += __shfl_xor(sum[b], 16);
-    sum[b] += __shfl_xor(sum[b], 32);
-    if (kq == 0) t.sums[(s0 / 64 + wm) * t.mc + l0 + wn * 64 + b * 16 + r16] = sum[b];
   }
 }
 
-// 128 features x 128 samples of the second product, over one share of the support vectors.  Features are the row
-// operand: a lane holds 4 consecutive ones of a sample.
-__global__ void __launch_bounds__(SBS, 4) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
-  __shared__ SplitStage S;
+// Shares of the support vectors in which the second product is done: those that leave the least of the chip idle in
+// the last round of workgroups (a CU's worth each), against 2% for the sums of each share.
+__device__ __forceinline__ int shares_of(const GradTiles &t, int64_t tiles, int64_t stages) {
+  int best = 1;
+  float cost = INFINITY;
+  for (int s = 1; s <= t.splits && (s == 1 || stages >= 16 * s); ++s) {
+    const float now = (float)((tiles * s + 255) / 256) / (float)s * (1.f + 0.02f * (float)s);
+    if (now < cost) {
+      cost = now;
+      best = s;
+    }
+  }
+  return best;
+}
+
+// Tiles of the second product (features x samples) of the samples q_first .. q_end - 1, and its shares.
+__device__ __forceinline__ int product_shares(const GradTiles &t, int64_t features, int64_t samples, int nsv) {
+  const int64_t nft = (features + 32 * t.fw - 1) / (32 * t.fw), nqt = (samples + ST - 1) / ST;
+  return shares_of(t, nft * nqt, (nsv + SKS - 1) / SKS);
+}
+
+// 32 FW features x 128 samples of the second product, over one share of the support vectors.  Features are the row
+// operand: a lane holds 4 consecutive ones of a sample.  The stages are those of split_tile.hpp with another
+// number of rows.
+template <int FW>
+__global__ void __launch_bounds__(SBS, FW == 5 ? 3 : 4) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+  constexpr int TF = 32 * FW, CH = FW + 4;  // features of the tile; 8-row chunks of a stage that each wave loads
+  __shared__ h8 S[(TF + ST) * 8];
   const int nsv = t.count[0];
   if (c.Q == nullptr) q_end = min(q_end, (int64_t)nsv);
   if (q_first >= q_end || nsv == 0) return;
-  const int64_t nft = (c.d + ST - 1) / ST, nqt = (q_end - q_first + ST - 1) / ST;
+  const int64_t nft = (c.d + TF) / TF, nqt = (q_end - q_first + ST - 1) / ST;
+  const int splits = product_shares(t, c.d + 1, q_end - q_first, nsv);
   int64_t item;
-  if (!xcd_item(nft * nqt * t.splits, blockIdx.x, item)) return;
+  if (!xcd_item(nft * nqt * splits, blockIdx.x, item)) return;
   const int split = __builtin_amdgcn_readfirstlane((int)(item / (nft * nqt)));
   const int64_t rem = item - (int64_t)split * nft * nqt;
   const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / nft)) * ST;
-  const int64_t f0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem % nft)) * ST;
+  const int64_t f0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem % nft)) * TF;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
-  const int64_t stages = (nsv + SKS - 1) / SKS, per = (stages + t.splits - 1) / t.splits;
+  const int ph = r16 * 8 + (kq ^ (r16 & 7)), pl = r16 * 8 + ((kq | 4) ^ (r16 & 7));
+  const int64_t stages = (nsv + SKS - 1) / SKS, per = (stages + splits - 1) / splits;
   const int64_t st0 = min(stages, split * per), st1 = min(stages, st0 + per);
-  const char *src[SCH];
-  if (st0 < st1) {
+  const char *src[CH];
 #pragma unroll
-    for (int q = 0; q < SCH; ++q) {
-      const int i = ((w & 1) * SCH + q) * 8 + (lane >> 3);
-      src[q] = (w < 2 ? split_src(t.xt, min<int64_t>(f0 + i, c.d - 1)) : split_src(t.p, l0 + i)) + st0 * 4 * SKS;
-    }
-    split_stage_load(S, src);
+  for (int q = 0; q < CH; ++q) {
+    const int i = (w * CH + q) * 8 + (lane >> 3);  // row of the stage: features, then samples
+    src[q] = (i < TF ? split_src(t.xt, min<int64_t>(f0 + i, c.d)) : split_src(t.p, l0 + i - TF)) + st0 * 4 * SKS;
   }
+  const auto load = [&]() {
+#pragma unroll
+    for (int q = 0; q < CH; ++q) {
+      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)src[q],
+                                       (__attribute__((address_space(3))) void *)&S[(w * CH + q) * 64], 16, 0, 0);
+      src[q] += 4 * SKS;
+    }
+  };
+  if (st0 < st1) load();
   // A sum over 15,000 support vectors is 1,400 roundings of a growing fp32 one after the other; cut every FOLD
   // stages it is a tenth of that, and the rest happens once a cut (the tile of sums stays in L2 between).
   int64_t st = st0;
   do {
-    v4f acc[4][4];
-    const int64_t more = min(st1 - st, (int64_t)FOLD);
-    if (more > 0) {
-      split_tile_loaded(S, src, more, wm, wn, acc);
-      if (st + more < st1) split_stage_load(S, src);
+    v4f acc[FW][4];
+#pragma unroll
+    for (int a = 0; a < FW; ++a)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
+    const int64_t cut = min(st1, st + FOLD);
+    for (int64_t i = st; i < cut; ++i) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads to LDS
+      __syncthreads();
+      h8 ah[FW], al[FW];
+#pragma unroll
+      for (int a = 0; a < FW; ++a) {
+        ah[a] = S[(wm * FW + a) * 128 + ph];
+        al[a] = S[(wm * FW + a) * 128 + pl];
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const h8 bh = S[(2 * FW + wn * 4 + b) * 128 + ph], bl = S[(2 * FW + wn * 4 + b) * 128 + pl];
+#pragma unroll
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bh, acc[a][b], 0, 0, 0);
+#pragma unroll
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bl, acc[a][b], 0, 0, 0);
+#pragma unroll
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[a], bh, acc[a][b], 0, 0, 0);
+      }
+      __syncthreads();  // the stage has been read
+      if (i + 1 < st1) load();
     }
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      const int64_t f = f0 + wm * 64 + a * 16 + 4 * kq;
+    for (int a = 0; a < FW; ++a) {
+      const int64_t f = f0 + (wm * FW + a) * 16 + 4 * kq;
       if (f >= t.dc) continue;
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         v4f *o = reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l0 + wn * 64 + b * 16 + r16) * t.dc + f]);
-        if (more <= 0) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
         if (st > st0) acc[a][b] += *o;
         *o = acc[a][b];
       }
@@ -791,30 +901,33 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   const int64_t l = (int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6), q = q_first + l;
   if (q >= q_end) return;
   const int ec = coef_exp(t);
+  const int ex = t.count[2];
   int es = 0;
   (void)frexpf(__int_as_float(t.count[1]), &es);
   const int64_t row = objective ? t.sv_row[q] : q;
   const double up = objective ? -(double)t.coef[q] : c.up ? c.up[q] : 1.0;
-  const double f = nsv ? ldexp(2.0 * c.gamma * up, ec) : 0.0;
-  const double scale = ldexp(1.0, es - W_EXP - X_EXP);
+  const double f = nsv ? 2.0 * c.gamma * up : 0.0;
+  // powers of two that the sums and the weights' sum were scaled by: c_j / 2^ec and x_j / 2^es each, or c_j x_j / 2^ex
+  const bool ones = !t.fb || c.d % 16;
+  const double scale = ldexp(1.0, (t.fb ? ec + es : ex) - W_EXP - X_EXP);
+  const double sscale = ldexp(1.0, ec - W_EXP - (ones ? X_EXP : 0));
+  const int splits = t.fb ? t.splits : nsv ? product_shares(t, c.d + 1, q_end - q_first, nsv) : 0;
   float s = 0.f;
-  const bool ones = t.fb && c.d % 16;
-  for (int64_t k = lane; nsv && k < (t.fb ? t.splits : (nsv + ST - 1) / ST * 2); k += 64)
-    s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
+  for (int k = lane; nsv && k < splits; k += 64) s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (t.fb) s *= ldexpf(1.0f, ones ? -W_EXP - X_EXP : -W_EXP);
+  const double sum = sscale * (double)s;
   const float *x = (objective ? c.X : c.Q) + row * c.d;
   for (int64_t at = 4 * lane; at < c.d; at += 256) {
     float xv[4], o[4] = {};
     load_n<4>(x + at, c.d - at, xv);
-    for (int k = 0; nsv && k < t.splits; ++k) {
+    for (int k = 0; nsv && k < splits; ++k) {
       const v4f v = *reinterpret_cast<const v4f *>(&t.part[((int64_t)k * t.mc + l) * t.dc + at]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] += v[e];
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - (double)s * (double)xv[e]));
+    for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - sum * (double)xv[e]));
     store_n<4>(c.out + row * c.d + at, c.d - at, o);
   }
 }
@@ -835,7 +948,7 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   SplitRows sv = split_rows_of(c.X, c.n, t.sv), q = split_rows_of(objective ? c.X : c.Q, objective ? 0 : c.m, t.q);
   sv.perm = t.sv_row;
   const int64_t svb = split_rows_blocks(sv), qb = split_rows_blocks(q);
-  hipLaunchKernelGGL(grad_split_k, dim3((unsigned)(svb + qb)), dim3(TB), 0, s, sv, q, c.d, t.count, (int32_t)svb);
+  hipLaunchKernelGGL(grad_split_k, dim3((unsigned)(svb + qb)), dim3(TB), 0, s, sv, q, c.d, t, (int32_t)svb);
   const float cexp = (float)(-c.gamma * 1.4426950408889634);
   if (objective) hipLaunchKernelGGL(grad_zero_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c);
   if (t.fb) {
@@ -857,14 +970,25 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
     hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, (int64_t)0, c.m);
     return hipGetLastError();
   }
-  if (div_up(c.d, 64) > 65535) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(grad_transpose_k, dim3((unsigned)(t.svp / 32), (unsigned)div_up(c.d, 64)), dim3(TB), 0, s, c.X, c.d, t);
+  if (c.d / 64 + 1 > 65535) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(grad_transpose_k, dim3((unsigned)(t.svp / 32), (unsigned)(c.d / 64 + 1)), dim3(TB), 0, s, c.X, c.d, t);
+  const int64_t nst = t.svp / ST;
+  const bool sym = objective && t.mc >= c.m;
   for (int64_t q0 = 0; q0 < c.m; q0 += t.mc) {
     const int64_t q1 = c.m - q0 < t.mc ? c.m : q0 + t.mc, nqt = div_up(q1 - q0, ST);
-    const int64_t wb = round_up(nqt * (t.svp / ST), 8), pb = round_up(nqt * div_up(c.d, ST) * t.splits, 8);
-    if (wb > 0x7fffffffLL || pb > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(grad_weights_k, dim3((unsigned)wb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
-    hipLaunchKernelGGL(grad_product_k, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+    const int64_t kb = round_up(sym ? nst * (nst + 1) / 2 : nqt * nst, 8);
+    const int64_t pb = round_up(nqt * div_up(c.d + 1, 32 * t.fw) * t.splits, 8);
+    if (kb > 0x7fffffffLL || pb > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (sym)
+      hipLaunchKernelGGL(grad_kernel_k<true>, dim3((unsigned)kb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
+    else
+      hipLaunchKernelGGL(grad_kernel_k<false>, dim3((unsigned)kb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
+    if (t.fw == 3)
+      hipLaunchKernelGGL(grad_product_k<3>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+    else if (t.fw == 4)
+      hipLaunchKernelGGL(grad_product_k<4>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+    else
+      hipLaunchKernelGGL(grad_product_k<5>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
     hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t, q0, q1);
   }
   return hipGetLastError();
