@@ -572,9 +572,9 @@ __device__ __forceinline__ int product_shares(const GradTiles &t, int64_t featur
 // operand: a lane holds 4 consecutive ones of a sample.  The stages are those of split_tile.hpp with another
 // number of rows.
 template <int FW>
-__global__ void __launch_bounds__(SBS, FW == 5 ? 3 : 4) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+__global__ void __launch_bounds__(SBS, 2) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
   constexpr int TF = 32 * FW, CH = FW + 4;  // features of the tile; 8-row chunks of a stage that each wave loads
-  __shared__ h8 S[(TF + ST) * 8];
+  __shared__ h8 S[2][(TF + ST) * 8];  // this stage and the next, on its way
   const int nsv = t.count[0];
   if (c.Q == nullptr) q_end = min(q_end, (int64_t)nsv);
   if (q_first >= q_end || nsv == 0) return;
@@ -597,15 +597,21 @@ __global__ void __launch_bounds__(SBS, FW == 5 ? 3 : 4) grad_product_k(SvGradCal
     const int i = (w * CH + q) * 8 + (lane >> 3);  // row of the stage: features, then samples
     src[q] = (i < TF ? split_src(t.xt, min<int64_t>(f0 + i, c.d)) : split_src(t.p, l0 + i - TF)) + st0 * 4 * SKS;
   }
-  const auto load = [&]() {
+  const auto load = [&](int buf) {
 #pragma unroll
     for (int q = 0; q < CH; ++q) {
       __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)src[q],
-                                       (__attribute__((address_space(3))) void *)&S[(w * CH + q) * 64], 16, 0, 0);
+                                       (__attribute__((address_space(3))) void *)&S[buf][(w * CH + q) * 64], 16, 0, 0);
       src[q] += 4 * SKS;
     }
   };
-  if (st0 < st1) load();
+  const auto landed = [&]() {  // this wave's loads to LDS, then every wave's; the other buffer has been read
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  int buf = 0;
+  if (st0 < st1) load(0);
+  landed();
   // A sum over 15,000 support vectors is 1,400 roundings of a growing fp32 one after the other; cut every FOLD
   // stages it is a tenth of that, and the rest happens once a cut (the tile of sums stays in L2 between).
   int64_t st = st0;
@@ -617,17 +623,16 @@ __global__ void __launch_bounds__(SBS, FW == 5 ? 3 : 4) grad_product_k(SvGradCal
       for (int b = 0; b < 4; ++b) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
     const int64_t cut = min(st1, st + FOLD);
     for (int64_t i = st; i < cut; ++i) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads to LDS
-      __syncthreads();
+      if (i + 1 < st1) load(buf ^ 1);
       h8 ah[FW], al[FW];
 #pragma unroll
       for (int a = 0; a < FW; ++a) {
-        ah[a] = S[(wm * FW + a) * 128 + ph];
-        al[a] = S[(wm * FW + a) * 128 + pl];
+        ah[a] = S[buf][(wm * FW + a) * 128 + ph];
+        al[a] = S[buf][(wm * FW + a) * 128 + pl];
       }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const h8 bh = S[(2 * FW + wn * 4 + b) * 128 + ph], bl = S[(2 * FW + wn * 4 + b) * 128 + pl];
+        const h8 bh = S[buf][(2 * FW + wn * 4 + b) * 128 + ph], bl = S[buf][(2 * FW + wn * 4 + b) * 128 + pl];
 #pragma unroll
         for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bh, acc[a][b], 0, 0, 0);
 #pragma unroll
@@ -635,8 +640,8 @@ __global__ void __launch_bounds__(SBS, FW == 5 ? 3 : 4) grad_product_k(SvGradCal
 #pragma unroll
         for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[a], bh, acc[a][b], 0, 0, 0);
       }
-      __syncthreads();  // the stage has been read
-      if (i + 1 < st1) load();
+      landed();
+      buf ^= 1;
     }
 #pragma unroll
     for (int a = 0; a < FW; ++a) {
