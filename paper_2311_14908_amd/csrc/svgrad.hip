@@ -562,56 +562,74 @@ __device__ __forceinline__ int shares_of(const GradTiles &t, int64_t tiles, int6
   return best;
 }
 
+constexpr int PQ = 256;  // samples of a tile of the second product
+
 // Tiles of the second product (features x samples) of the samples q_first .. q_end - 1, and its shares.
 __device__ __forceinline__ int product_shares(const GradTiles &t, int64_t features, int64_t samples, int nsv) {
-  const int64_t nft = (features + 32 * t.fw - 1) / (32 * t.fw), nqt = (samples + ST - 1) / ST;
+  const int64_t nft = (features + 32 * t.fw - 1) / (32 * t.fw), nqt = (samples + PQ - 1) / PQ;
   return shares_of(t, nft * nqt, (nsv + SKS - 1) / SKS);
 }
 
-// 32 FW features x 128 samples of the second product, over one share of the support vectors.  Features are the row
-// operand: a lane holds 4 consecutive ones of a sample.  The stages are those of split_tile.hpp with another
-// number of rows.
+// 32 FW features x 256 samples of the second product, over one share of the support vectors; eight waves, each 16 FW
+// features x 64 samples.  Features are the row operand: a lane holds 4 consecutive ones of a sample.  A stage's
+// rows stand in LDS as in split_tile.hpp.  Three stages are in LDS: while one is multiplied the next one has
+// landed by half time (the only barrier of a stage), its feature operands are read during the second half, and
+// the one after is on its way.
+constexpr int PB = 512;
+
 template <int FW>
-__global__ void __launch_bounds__(SBS, 2) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
-  constexpr int TF = 32 * FW, CH = FW + 4;  // features of the tile; 8-row chunks of a stage that each wave loads
-  __shared__ h8 S[2][(TF + ST) * 8];  // this stage and the next, on its way
+__global__ void __launch_bounds__(PB, 1) grad_product_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+  constexpr int TF = 32 * FW, CHUNKS = (TF + PQ) / 8, CH = (CHUNKS + 7) / 8;  // 8-row chunks of a stage, and each wave's
+  __shared__ h8 S[3][(TF + PQ) * 8];
   const int nsv = t.count[0];
   if (c.Q == nullptr) q_end = min(q_end, (int64_t)nsv);
   if (q_first >= q_end || nsv == 0) return;
-  const int64_t nft = (c.d + TF) / TF, nqt = (q_end - q_first + ST - 1) / ST;
+  const int64_t nft = (c.d + TF) / TF, nqt = (q_end - q_first + PQ - 1) / PQ;
   const int splits = product_shares(t, c.d + 1, q_end - q_first, nsv);
   int64_t item;
   if (!xcd_item(nft * nqt * splits, blockIdx.x, item)) return;
   const int split = __builtin_amdgcn_readfirstlane((int)(item / (nft * nqt)));
   const int64_t rem = item - (int64_t)split * nft * nqt;
-  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / nft)) * ST;
+  const int64_t l0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / nft)) * PQ;
   const int64_t f0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem % nft)) * TF;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = w >> 1, wn = w & 1, kq = lane >> 4, r16 = lane & 15;
+  const int wm = w >> 2, wn = w & 3, kq = lane >> 4, r16 = lane & 15;
   const int ph = r16 * 8 + (kq ^ (r16 & 7)), pl = r16 * 8 + ((kq | 4) ^ (r16 & 7));
   const int64_t stages = (nsv + SKS - 1) / SKS, per = (stages + splits - 1) / splits;
   const int64_t st0 = min(stages, split * per), st1 = min(stages, st0 + per);
   const char *src[CH];
 #pragma unroll
   for (int q = 0; q < CH; ++q) {
-    const int i = (w * CH + q) * 8 + (lane >> 3);  // row of the stage: features, then samples
-    src[q] = (i < TF ? split_src(t.xt, min<int64_t>(f0 + i, c.d)) : split_src(t.p, l0 + i - TF)) + st0 * 4 * SKS;
+    const int i = min(w + 8 * q, CHUNKS - 1) * 8 + (lane >> 3);  // row of the stage: features, then samples
+    src[q] = (i < TF ? split_src(t.xt, min<int64_t>(f0 + i, c.d)) : split_src(t.p, min<int64_t>(l0 + i - TF, t.mc - 1))) +
+             st0 * 4 * SKS;
   }
   const auto load = [&](int buf) {
 #pragma unroll
     for (int q = 0; q < CH; ++q) {
-      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)src[q],
-                                       (__attribute__((address_space(3))) void *)&S[buf][(w * CH + q) * 64], 16, 0, 0);
+      if (w + 8 * q < CHUNKS)
+        __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) const void *)src[q],
+                                         (__attribute__((address_space(3))) void *)&S[buf][(w + 8 * q) * 64], 16, 0, 0);
       src[q] += 4 * SKS;
     }
   };
-  const auto landed = [&]() {  // this wave's loads to LDS, then every wave's; the other buffer has been read
+  const auto landed = [&]() {  // this wave's loads to LDS, then every wave's
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  int buf = 0;
+  h8 ah[FW], al[FW];
+  const auto features = [&](int buf, h8 (&h)[FW], h8 (&l)[FW]) {
+#pragma unroll
+    for (int a = 0; a < FW; ++a) {
+      h[a] = S[buf][(wm * FW + a) * 128 + ph];
+      l[a] = S[buf][(wm * FW + a) * 128 + pl];
+    }
+  };
+  int buf = 0;  // this stage's
   if (st0 < st1) load(0);
   landed();
+  if (st0 + 1 < st1) load(1);
+  if (st0 < st1) features(0, ah, al);
   // A sum over 15,000 support vectors is 1,400 roundings of a growing fp32 one after the other; cut every FOLD
   // stages it is a tenth of that, and the rest happens once a cut (the tile of sums stays in L2 between).
   int64_t st = st0;
@@ -623,15 +641,7 @@ __global__ void __launch_bounds__(SBS, 2) grad_product_k(SvGradCall c, GradTiles
       for (int b = 0; b < 4; ++b) acc[a][b] = (v4f){0.f, 0.f, 0.f, 0.f};
     const int64_t cut = min(st1, st + FOLD);
     for (int64_t i = st; i < cut; ++i) {
-      if (i + 1 < st1) load(buf ^ 1);
-      h8 ah[FW], al[FW];
-#pragma unroll
-      for (int a = 0; a < FW; ++a) {
-        ah[a] = S[buf][(wm * FW + a) * 128 + ph];
-        al[a] = S[buf][(wm * FW + a) * 128 + pl];
-      }
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      const auto multiply = [&](int b) {
         const h8 bh = S[buf][(2 * FW + wn * 4 + b) * 128 + ph], bl = S[buf][(2 * FW + wn * 4 + b) * 128 + pl];
 #pragma unroll
         for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bh, acc[a][b], 0, 0, 0);
@@ -639,9 +649,22 @@ __global__ void __launch_bounds__(SBS, 2) grad_product_k(SvGradCall c, GradTiles
         for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bl, acc[a][b], 0, 0, 0);
 #pragma unroll
         for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[a], bh, acc[a][b], 0, 0, 0);
+      };
+      const int next = buf == 2 ? 0 : buf + 1, after = next == 2 ? 0 : next + 1;
+      multiply(0);
+      multiply(1);
+      landed();  // the next stage; everyone is done with the stage before this one
+      if (i + 2 < st1) load(after);
+      h8 nh[FW], nl[FW];
+      features(next, nh, nl);  // (past the last stage: what the buffer holds, not used)
+      multiply(2);
+      multiply(3);
+#pragma unroll
+      for (int a = 0; a < FW; ++a) {
+        ah[a] = nh[a];
+        al[a] = nl[a];
       }
-      landed();
-      buf ^= 1;
+      buf = next;
     }
 #pragma unroll
     for (int a = 0; a < FW; ++a) {
@@ -649,7 +672,9 @@ __global__ void __launch_bounds__(SBS, 2) grad_product_k(SvGradCall c, GradTiles
       if (f >= t.dc) continue;
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        v4f *o = reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l0 + wn * 64 + b * 16 + r16) * t.dc + f]);
+        const int64_t l = l0 + wn * 64 + b * 16 + r16;
+        if (l >= t.mc) continue;
+        v4f *o = reinterpret_cast<v4f *>(&t.part[((int64_t)split * t.mc + l) * t.dc + f]);
         if (st > st0) acc[a][b] += *o;
         *o = acc[a][b];
       }
@@ -982,18 +1007,18 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   for (int64_t q0 = 0; q0 < c.m; q0 += t.mc) {
     const int64_t q1 = c.m - q0 < t.mc ? c.m : q0 + t.mc, nqt = div_up(q1 - q0, ST);
     const int64_t kb = round_up(sym ? nst * (nst + 1) / 2 : nqt * nst, 8);
-    const int64_t pb = round_up(nqt * div_up(c.d + 1, 32 * t.fw) * t.splits, 8);
+    const int64_t pb = round_up(div_up(q1 - q0, PQ) * div_up(c.d + 1, 32 * t.fw) * t.splits, 8);
     if (kb > 0x7fffffffLL || pb > 0x7fffffffLL) return hipErrorInvalidValue;
     if (sym)
       hipLaunchKernelGGL(grad_kernel_k<true>, dim3((unsigned)kb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
     else
       hipLaunchKernelGGL(grad_kernel_k<false>, dim3((unsigned)kb), dim3(SBS), 0, s, c, t, cexp, q0, q1);
     if (t.fw == 3)
-      hipLaunchKernelGGL(grad_product_k<3>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+      hipLaunchKernelGGL(grad_product_k<3>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
     else if (t.fw == 4)
-      hipLaunchKernelGGL(grad_product_k<4>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+      hipLaunchKernelGGL(grad_product_k<4>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
     else
-      hipLaunchKernelGGL(grad_product_k<5>, dim3((unsigned)pb), dim3(SBS), 0, s, c, t, q0, q1);
+      hipLaunchKernelGGL(grad_product_k<5>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
     hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t, q0, q1);
   }
   return hipGetLastError();
