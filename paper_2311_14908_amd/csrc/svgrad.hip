@@ -3,7 +3,7 @@
 // out_q = u_q 2 gamma sum_j c_j K(x_j, x_q) (x_j - x_q), c_j = a_j y_j.  The objective's gradient is the same
 // sum with the rows themselves as samples and u_q = -c_q (a_j y_j a_q y_q K is symmetric, which cancels the
 // 1/2), zero where a_q = 0; the pair j = q adds nothing and is left out.
-// Up to 16 samples of up to 1,024 features take a pass over the training rows.  More take two products in tiles on
+// A few samples (few_most) of up to 1,024 features take a pass over the training rows.  More take two products in tiles on
 // the fp16 matrix cores with fp32 accuracy (split_tile.hpp).  Rows of up to 128 features keep the kernel values
 // between them in registers (grad_short_k), longer ones in HBM:
 //   1. grad_compact_k: the support vectors in index order, their c_j, its largest magnitude;
@@ -29,7 +29,12 @@ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int GB = 256, GU = 4;  // threads, units of four features a lane holds of a row
 constexpr int GL = 256;          // training rows looked at in one go
-constexpr int64_t FEW_M = 16, FEW_D = 4LL * GU * 64;  // samples and features the pass takes
+constexpr int64_t FEW_D = 4LL * GU * 64;  // features the pass takes
+
+// Samples the pass takes: it costs about as much for every four, the tiles cost their preparation first.  Us a call
+// (pass, tiles), 60% support vectors: 16 samples against 20,000 x 784 91, 188; 32 166, 189; 64 316, 190; 32
+// against 300,000 x 64 189, 349; against 100,000 x 31 16 93, 124, but 32 176, 125.
+constexpr int64_t few_most(int64_t d) { return d >= 64 ? 32 : 16; }
 
 // Chunks of training rows: 32 rows each, at most 512 of them.
 int64_t few_chunks(int64_t n) {
@@ -174,13 +179,13 @@ __global__ void __launch_bounds__(GB) sv_grad_few_join_k(SvGradCall c, int64_t c
   store_n<4>(c.out + q * c.d + at, c.d - at, s);
 }
 
-bool takes_pass(int64_t d, int64_t m) { return m <= FEW_M && d <= FEW_D; }
+bool takes_pass(int64_t d, int64_t m) { return m <= few_most(d) && d <= FEW_D; }
 
 hipError_t launch_few(const SvGradCall &c, void *ws, hipStream_t s) {
   const int64_t chunks = few_chunks(c.n), per = div_up(c.n, chunks), dc = div_up(c.d, 4) * 4;
   float *part = reinterpret_cast<float *>((reinterpret_cast<uintptr_t>(ws) + 255) & ~(uintptr_t)255);
-  int gs = 1;
-  while (gs < 64 && 4LL * GU * gs < c.d) gs <<= 1;
+  int gs = 1;  // as few lanes as hold a row, but no more row groups than rows in a chunk
+  while (gs < 64 && (4LL * GU * gs < c.d || GB / gs > per)) gs <<= 1;
   const size_t lds = (size_t)(GB / gs) * dc * 4;
   const double cexp = -c.gamma * 1.4426950408889634;
   const dim3 grid((unsigned)chunks, (unsigned)(c.m == 1 ? 1 : div_up(c.m, 4)));
