@@ -23,20 +23,21 @@ constexpr int64_t RANK_MAX = 8192;  // positions sorted by counting smaller ones
 constexpr int SB = 512;             // threads of a workgroup of the sort
 constexpr int SORT_BLOCKS = 256;
 constexpr int DIGIT_MAX = 9;        // bits of a pass of the sort at most
-constexpr int SPAN = 32;            // chunks of a run that one thread joins
+constexpr int SPAN = 32, RUN_SPAN = 8;  // chunks that one thread joins: of a bag, of a token's run
 
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Positions of a chunk: about 2^18 threads of 8 values each, between 16 positions (below, the joins cost
 // more than the rows) and 128 (above, nothing is gained).
 // Up to 64 positions are one chunk: a second launch costs more than they do.
-int64_t chunk_of(int64_t T, int64_t d) {
-  if (T <= 64) return 64;
+int chunk_log(int64_t T, int64_t d) {
+  if (T <= 64) return 6;
   const double want = (double)T * (double)div_up(d, 8) / 131072.0;
-  int64_t L = 16;
-  while (L < 128 && (double)L < want) L <<= 1;
-  return L;
+  int lg = 4;
+  while (lg < 7 && (double)(1 << lg) < want) ++lg;
+  return lg;
 }
+int64_t chunk_of(int64_t T, int64_t d) { return 1ll << chunk_log(T, d); }
 
 // Token i.  Both widths are read as 32-bit words without a branch (a 64-bit token's second word, else the one word
 // again), so that the loads of several tokens are under way at once.
@@ -108,7 +109,8 @@ struct Columns {
 
 // Item of this thread: `of` = which chunk or row, `unit` = which 16 bytes of it.
 __device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &unit) {
-  const int64_t b0 = (int64_t)blockIdx.x * EB, c0 = b0 / units;
+  // (a 64-bit division costs a hundred instructions)
+  const int64_t b0 = (int64_t)blockIdx.x * EB, c0 = b0 >> 32 ? b0 / units : (int64_t)((uint32_t)b0 / (uint32_t)units);
   const uint32_t r = (uint32_t)(b0 - c0 * units) + threadIdx.x;
   of = c0 + r / (uint32_t)units;
   unit = r % (uint32_t)units;
@@ -181,8 +183,9 @@ struct Parts {
 // empty one at the very end to the last chunk.
 template <int N, bool SMALL, class TE>
 __global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
-                                                   int32_t out_type, int64_t ld_out, int64_t units, int64_t L,
+                                                   int32_t out_type, int64_t ld_out, int64_t units, int lg,
                                                    int64_t chunks, Parts part) {
+  const int64_t L = 1ll << lg;
   int64_t ch, unit;
   item_of(units, ch, unit);
   if (ch >= chunks) return;
@@ -269,7 +272,8 @@ __device__ __forceinline__ void join_long(const float *__restrict__ part, int64_
 // earlier such chunk has it.
 template <int N, bool SMALL>
 __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32_t out_type, int64_t ld_out, int64_t units,
-                                                   int64_t L, int64_t chunks, int64_t short_blocks, Parts part) {
+                                                   int lg, int64_t chunks, int64_t short_blocks, Parts part) {
+  const int64_t L = 1ll << lg;
   __shared__ float lds[JS][JU][N];
   __shared__ int counts[EB / 64];
   int64_t ch, unit, b, last;
@@ -280,7 +284,7 @@ __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32
     if (ch >= chunks) return;
     b = part.tail[ch];
     if (b < 0) return;
-    last = (min(c.bags[b + 1], c.T) - 1) / L;
+    last = (min(c.bags[b + 1], c.T) - 1) >> lg;
     if (last - ch >= SPAN) return;
     join_short<N>(part.sum, units, unit, ch, last, acc);
     used = part.used[ch * 2 + 1];
@@ -290,8 +294,8 @@ __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32
     if (x >= chunks) return;
     b = lower_bound<int64_t>(c.bags, c.B + 1, x * L) - 1;
     if (b < 0 || b >= c.B || c.bags[b] < 0 || c.bags[b + 1] <= x * L) return;
-    ch = c.bags[b] / L;
-    last = (min(c.bags[b + 1], c.T) - 1) / L;
+    ch = c.bags[b] >> lg;
+    last = (min(c.bags[b + 1], c.T) - 1) >> lg;
     if (last - ch < SPAN || ch < x - SPAN) return;
     unit = i % groups * JU + threadIdx.x % JU;
     for (int64_t k = threadIdx.x; k <= last - ch; k += EB) used += part.used[(ch + k) * 2 + (k == 0 ? 1 : 0)];
@@ -391,10 +395,11 @@ struct FillCall {
 };
 
 // Up to RANK_MAX positions: the place of a position is the number of positions with a smaller token, or the
-// same token and a smaller index.  16 positions a workgroup, 16 lanes a position that take every 16th
-// four of the others (their LDS reads are one after the other in memory), and look for its bag among 16 starts
+// same token and a smaller index.  8 positions a workgroup, 32 lanes a position that take every 32nd
+// four of the others (their LDS reads are one after the other in memory), and look for its bag among 32 starts
 // at a time.  Blocks past the sort's zero dE meanwhile.
-constexpr int RP = 16, RS = EB / RP;
+constexpr int RP = 8, RS = EB / RP;
+static_assert(RP % 4 == 0 && RS >= RP, "embed_rank_k");
 
 __device__ __forceinline__ int group_sum(int v) {
 #pragma unroll
@@ -402,12 +407,19 @@ __device__ __forceinline__ int group_sum(int v) {
   return v;
 }
 
+// How many of four keys are smaller than k, all of them below 2^31: by sign bits (comparisons that are added up through
+// the carry wait for it).
+__device__ __forceinline__ int below(const uint32_t *o4, uint32_t k) {
+  const uint4 o = *reinterpret_cast<const uint4 *>(o4);
+  return (int)(((o.x - k) >> 31) + ((o.y - k) >> 31) + ((o.z - k) >> 31) + ((o.w - k) >> 31));
+}
+
 __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, FillCall f, int64_t sort_blocks) {
   if ((int64_t)blockIdx.x >= sort_blocks) {
     zero_rows(f.de, f.type, f.rows, f.d, f.ld, blockIdx.x - sort_blocks, f.blocks);
     return;
   }
-  extern __shared__ uint32_t keys[];
+  extern __shared__ __align__(16) uint32_t keys[];
   const int T = (int)c.T, pos = threadIdx.x / RS, sl = threadIdx.x % RS;
   const int Tp = (T + 4 * RS - 1) / (4 * RS) * (4 * RS);
   for (int j0 = threadIdx.x; j0 < Tp; j0 += 16 * EB) {
@@ -420,12 +432,12 @@ __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, Fil
       const uint32_t k = c.padding >= 0 && t[q] == c.padding ? (uint32_t)c.V
                          : (uint64_t)t[q] >= (uint64_t)c.V   ? (uint32_t)c.V + 1
                                                              : (uint32_t)t[q];
-      if (j < Tp) keys[j] = j < T ? k : 0xffffffffu;
+      if (j < Tp) keys[j] = j < T ? k : 0x7fffffffu;
     }
   }
   const int p0 = blockIdx.x * RP, i = p0 + pos;
   int64_t b = i, s0 = 0, s1 = 0;
-  if (c.bags) {  // the last bag that starts at i or before: between lo and hi, a sixteenth of which is left each time
+  if (c.bags) {  // the last bag that starts at i or before: between lo and hi, one part in 32 of which is left each time
     int64_t lo = 0, hi = c.B;
     while (hi - lo > 1) {
       const int64_t step = (hi - lo + RS - 1) / RS, at = lo + (sl + 1) * step;
@@ -439,16 +451,12 @@ __global__ void __launch_bounds__(EB) embed_rank_k(EmbedCall c, GradSpace g, Fil
   }
   __syncthreads();
   const uint32_t k = i < T ? keys[i] : 0u;
-  int rank = 0;
-#pragma unroll 8
-  for (int j = 4 * sl; j < Tp; j += 4 * RS) {
-    const uint4 o = *reinterpret_cast<const uint4 *>(&keys[j]);
-    // (o <= k) before the workgroup's positions, (o < k) after them, by index in between
-    const uint32_t before = j + 4 <= p0 ? k + 1 : k;
-    rank += (o.x < before) + (o.y < before) + (o.z < before) + (o.w < before);
-    if (j + 4 > p0 && j < p0 + RP)
-      rank += (o.x == k && j < i) + (o.y == k && j + 1 < i) + (o.z == k && j + 2 < i) + (o.w == k && j + 3 < i);
-  }
+  int rank = 0, j = 4 * sl;
+#pragma unroll 4
+  for (; j < p0; j += 4 * RS) rank += below(&keys[j], k + 1);  // before the workgroup's positions: smaller or the same
+#pragma unroll 4
+  for (; j < Tp; j += 4 * RS) rank += below(&keys[j], k);  // from there on: smaller
+  if (sl < pos) rank += keys[p0 + sl] == k;  // the same, among the workgroup's own
   rank = group_sum(rank);
   // the first position of a bag counts the bag's that are not padding
   int used = 0;
@@ -621,8 +629,9 @@ template <int N, bool SMALL, class TY>
 __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *__restrict__ key,
                                                    const uint32_t *__restrict__ src, const int32_t *__restrict__ count,
                                                    const TY *__restrict__ dy, int64_t ld, void *de, int32_t de_type,
-                                                   int64_t ld_de, int32_t accumulate, int64_t units, int64_t L,
+                                                   int64_t ld_de, int32_t accumulate, int64_t units, int lg,
                                                    int64_t chunks, float *__restrict__ part) {
+  const int64_t L = 1ll << lg;
   int64_t ch, unit;
   item_of(units, ch, unit);
   if (ch >= chunks) return;
@@ -689,8 +698,9 @@ __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *
 template <int N, bool SMALL>
 __global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint32_t *__restrict__ key, void *de,
                                                         int32_t de_type, int64_t ld_de, int32_t accumulate,
-                                                        int64_t units, int64_t L, int64_t chunks, int64_t short_blocks,
+                                                        int64_t units, int lg, int64_t chunks, int64_t short_blocks,
                                                         const float *__restrict__ part) {
+  const int64_t L = 1ll << lg;
   __shared__ float lds[JS][JU][N];
   int64_t ch, unit;
   uint32_t run;
@@ -701,24 +711,29 @@ __global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint3
     if (ch >= chunks || i1 >= c.T) return;
     run = key[i1];
     if (run >= (uint32_t)c.V || key[i1 - 1] != run || (i0 > 0 && key[i0 - 1] == run)) return;
-    int64_t last = ch + 1;  // the last chunk that starts inside the run (the keys are sorted: count them)
-    for (int64_t k = ch + 2; k <= ch + SPAN; k += 8) {
-      int more = 0;
+    // the last chunk that starts inside the run (the keys are sorted: count the starts that are in it)
+    int64_t last = ch + 1;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) more += k + q <= ch + SPAN && key[min((k + q) * L, c.T - 1)] == run && (k + q) * L < c.T;
-      last += more;
-      if (more < 8) break;
-    }
-    if (last - ch >= SPAN) return;
+    for (int q = 2; q <= RUN_SPAN; ++q) last += (ch + q) * L < c.T && key[min((ch + q) * L, c.T - 1)] == run;
+    if (last - ch >= RUN_SPAN) return;
     join_short<N>(part, units, unit, ch, last, acc);
   } else {
-    const int64_t i = blockIdx.x - short_blocks, groups = (units + JU - 1) / JU, x = (i / groups + 1) * SPAN;
+    const int64_t i = blockIdx.x - short_blocks, groups = (units + JU - 1) / JU, x = (i / groups + 1) * RUN_SPAN;
     if (x >= chunks) return;
     run = key[x * L];
     if (run >= (uint32_t)c.V || key[x * L - 1] != run) return;
-    ch = lower_bound<uint32_t>(key, x * L, run) / L;
-    const int64_t last = (x * L + lower_bound<uint32_t>(key + x * L, c.T - x * L, run + 1) - 1) / L;
-    if (last - ch < SPAN || ch < x - SPAN) return;
+    // chunks after x, and from x back, that start inside the run, a workgroup's width at a time
+    int64_t last = x, first = x;
+    for (int n = EB; n == EB; last += n) {
+      const int64_t at = (last + 1 + threadIdx.x) * L;
+      n = __syncthreads_count(at < c.T && key[min(at, c.T - 1)] == run);
+    }
+    for (int n = EB; n == EB; first -= n) {
+      const int64_t at = (first - 1 - (int64_t)threadIdx.x) * L;
+      n = __syncthreads_count(at >= 0 && key[at < 0 ? 0 : at] == run);
+    }
+    ch = first > 0 && key[first * L - 1] == run ? first - 1 : first;
+    if (last - ch < RUN_SPAN || ch < x - RUN_SPAN) return;
     unit = i % groups * JU + threadIdx.x % JU;
     join_long<N>(part, units, unit, ch, last, acc, lds);
     if (threadIdx.x >= JU || unit >= units) return;
@@ -760,9 +775,9 @@ bool grid_fits(int64_t blocks) { return blocks <= 0x7fffffffLL; }
 int64_t part_floats(int64_t T, int64_t d) { return div_up(T > 0 ? T : 1, chunk_of(T, d)) * 2 * div_up(d, 8) * 8; }
 
 // Blocks of a join: those for short runs, and all.
-void join_blocks(int64_t chunks, int64_t units, int64_t &shorts, int64_t &all) {
+void join_blocks(int64_t chunks, int64_t units, int span, int64_t &shorts, int64_t &all) {
   shorts = div_up(chunks * units, EB);
-  all = shorts + (chunks - 1) / SPAN * div_up(units, JU);
+  all = shorts + (chunks - 1) / span * div_up(units, JU);
 }
 
 template <class P>
@@ -800,19 +815,20 @@ hipError_t launch_embed(const EmbedCall &c, const void *table, int32_t table_typ
                          ld_out, units);
       return hipGetLastError();
     }
-    const int64_t L = chunk_of(c.T, c.d), chunks = c.T > 0 ? div_up(c.T, L) : 1;
+    const int lg = chunk_log(c.T, c.d);
+    const int64_t chunks = c.T > 0 ? div_up(c.T, 1ll << lg) : 1;
     int64_t shorts, all;
-    join_blocks(chunks, units, shorts, all);
+    join_blocks(chunks, units, SPAN, shorts, all);
     if (!grid_fits(all)) return hipErrorInvalidValue;
     Parts part;
     part.sum = aligned<float>(ws);
     part.used = reinterpret_cast<int32_t *>(part.sum + chunks * 2 * units * N);
     part.tail = part.used + 2 * chunks;
     hipLaunchKernelGGL((embed_bags_k<N, SMALL, TE>), dim3((unsigned)shorts), dim3(EB), 0, s, c, E, ld_table, out, out_type,
-                       ld_out, units, L, chunks, part);
+                       ld_out, units, lg, chunks, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks == 1) return e;
-    hipLaunchKernelGGL((embed_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, out, out_type, ld_out, units, L,
+    hipLaunchKernelGGL((embed_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, out, out_type, ld_out, units, lg,
                        chunks, shorts, part);
     return hipGetLastError();
   });
@@ -861,17 +877,18 @@ hipError_t launch_embed_grad(const EmbedCall &c, const void *dy, int32_t dy_type
     using TY = std::remove_cv_t<std::remove_pointer_t<decltype(tag)>>;
     constexpr int N = UNIT<TY>;
     constexpr bool SMALL = decltype(small)::value;
-    const int64_t units = div_up(c.d, N), L = chunk_of(c.T, c.d), chunks = div_up(c.T, L);
+    const int lg = chunk_log(c.T, c.d);
+    const int64_t units = div_up(c.d, N), chunks = div_up(c.T, 1ll << lg);
     int64_t shorts, all;
-    join_blocks(chunks, units, shorts, all);
+    join_blocks(chunks, units, RUN_SPAN, shorts, all);
     if (!grid_fits(all)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((embed_runs_k<N, SMALL, TY>), dim3((unsigned)shorts), dim3(EB), 0, s, c, g.key[cur], g.src[cur],
-                       g.count, static_cast<const TY *>(dy), ld_dy, de, de_type, ld_de, accumulate ? 1 : 0, units, L, chunks,
+                       g.count, static_cast<const TY *>(dy), ld_dy, de, de_type, ld_de, accumulate ? 1 : 0, units, lg, chunks,
                        g.part);
     hipError_t e2 = hipGetLastError();
     if (e2 != hipSuccess || chunks == 1) return e2;
     hipLaunchKernelGGL((embed_runs_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, g.key[cur], de, de_type, ld_de,
-                       accumulate ? 1 : 0, units, L, chunks, shorts, g.part);
+                       accumulate ? 1 : 0, units, lg, chunks, shorts, g.part);
     return hipGetLastError();
   });
 }

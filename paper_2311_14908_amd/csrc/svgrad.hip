@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(SBS, 3) grad_kernel_k(SvGradCall c, GradTiles 
 __device__ __forceinline__ int shares_of(const GradTiles &t, int64_t tiles, int64_t stages) {
   int best = 1;
   float cost = INFINITY;
-  for (int s = 1; s <= t.splits && (s == 1 || stages >= 16 * s); ++s) {
+  for (int s = 1; s <= t.splits && (s == 1 || stages >= 4 * s); ++s) {
     const float now = (float)((tiles * s + 255) / 256) / (float)s * (1.f + 0.02f * (float)s);
     if (now < cost) {
       cost = now;
@@ -946,9 +946,9 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   const bool ones = !t.fb || c.d % 16;
   const double scale = ldexp(1.0, (t.fb ? ec + es : ex) - W_EXP - X_EXP);
   const double sscale = ldexp(1.0, ec - W_EXP - (ones ? X_EXP : 0));
-  const int splits = t.fb ? t.splits : nsv ? product_shares(t, c.d + 1, q_end - q_first, nsv) : 0;
+  const int splits = !nsv ? 0 : t.fb ? t.splits : product_shares(t, c.d + 1, q_end - q_first, nsv);
   float s = 0.f;
-  for (int k = lane; nsv && k < splits; k += 64) s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
+  for (int k = lane; k < splits; k += 64) s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   const double sum = sscale * (double)s;
@@ -956,7 +956,8 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   for (int64_t at = 4 * lane; at < c.d; at += 256) {
     float xv[4], o[4] = {};
     load_n<4>(x + at, c.d - at, xv);
-    for (int k = 0; nsv && k < splits; ++k) {
+#pragma unroll 8
+    for (int k = 0; k < splits; ++k) {
       const v4f v = *reinterpret_cast<const v4f *>(&t.part[((int64_t)k * t.mc + l) * t.dc + at]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] += v[e];

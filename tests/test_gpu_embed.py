@@ -264,3 +264,34 @@ def test_binding_refusals():
                 lambda: svmx.svm_embed_grad(tok, table, 9), lambda: svmx.svm_embed_grad(tok, table[:3], 9, out=table[:5])):
         with pytest.raises((TypeError, ValueError)):
             bad()
+
+
+@pytest.mark.parametrize("T,d", [(40000, 8), (9000, 1), (70001, 33)])
+def test_runs_of_thousands_of_chunks(T, d):
+    """One bag of all tokens, and one token in all places (then two): runs far longer than a workgroup's width of chunks."""
+    starts = torch.tensor([0, 0, T, T])
+    g = torch.Generator().manual_seed(T)
+    tok = torch.randint(0, 30, (T,), generator=g).to(torch.int32)
+    table = torch.randn(30, d, generator=g)
+    ref, err = forward64(table, tok, starts, 1.0, True, 5)
+    close(svmx.svm_embed(table.cuda(), tok.cuda(), bags=starts.cuda(), mean=True, padding=5), ref, err)
+    dy = torch.randn(T, d, generator=g)
+    for cut in (0, T // 3, T - 1):
+        tok = torch.full((T,), 7, dtype=torch.int32)
+        tok[:cut] = 3
+        ref, err = grad64(tok, dy, 9, torch.arange(T + 1), 1.0, False, -1)
+        close(svmx.svm_embed_grad(tok.cuda(), dy.cuda(), 9), ref, err)
+
+
+def test_long_bags_among_short_ones():
+    """Bags of about two tokens, empty ones, and here and there one that many chunks hold."""
+    lens = [k % 4 for k in range(4000)]
+    for at, n in ((0, 300), (500, 65), (1000, 64), (1001, 63), (1700, 129), (1701, 128), (2600, 900), (3999, 257)):
+        lens[at] = n
+    for dtype, d in ((torch.float32, 20), (torch.bfloat16, 61)):
+        for mean, padding in ((True, 3), (False, -1)):
+            tok, starts = make(90, d, lens, 4, padding=padding)
+            table = torch.randn(90, d, generator=torch.Generator().manual_seed(5)).to(dtype)
+            ref, err = forward64(table, tok, starts, 1.5, mean, padding)
+            close(svmx.svm_embed(table.cuda(), tok.cuda(), bags=starts.cuda(), scale=1.5, mean=mean, padding=padding,
+                                 out_dtype=torch.float32), ref, err)
