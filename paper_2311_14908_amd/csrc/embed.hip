@@ -108,9 +108,9 @@ struct Columns {
 };
 
 // Item of this thread: `of` = which chunk or row, `unit` = which 16 bytes of it.
-__device__ __forceinline__ void item_of(int64_t units, int64_t &of, int64_t &unit) {
+__device__ __forceinline__ void item_of(int64_t block, int64_t units, int64_t &of, int64_t &unit) {
   // (a 64-bit division costs a hundred instructions)
-  const int64_t b0 = (int64_t)blockIdx.x * EB, c0 = b0 >> 32 ? b0 / units : (int64_t)((uint32_t)b0 / (uint32_t)units);
+  const int64_t b0 = block * EB, c0 = b0 >> 32 ? b0 / units : (int64_t)((uint32_t)b0 / (uint32_t)units);
   const uint32_t r = (uint32_t)(b0 - c0 * units) + threadIdx.x;
   of = c0 + r / (uint32_t)units;
   unit = r % (uint32_t)units;
@@ -159,7 +159,7 @@ template <int N, bool SMALL, class TE>
 __global__ void __launch_bounds__(EB) embed_rows_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
                                                    int32_t out_type, int64_t ld_out, int64_t units) {
   int64_t row, unit;
-  item_of(units, row, unit);
+  item_of(blockIdx.x, units, row, unit);
   if (row >= c.T) return;
   const Columns<N, SMALL> col(unit, c.d);
   const int64_t t = token_at(c, row);
@@ -179,48 +179,82 @@ struct Parts {
   int32_t *tail;  // forward: the bag that begins in the chunk and goes on after it, or -1
 };
 
+// The positions of bag b in chunk i0 .. i1 - 1 of the thread's unit: to the bag's row, or, where the bag crosses an end
+// of the chunk, to the chunk's partial sums.  Returns whether it goes on after the chunk.
+template <int N, bool SMALL, class TE>
+__device__ __forceinline__ bool sum_bag(const EmbedCall &c, const TE *__restrict__ E, int64_t ld, void *out, int32_t out_type,
+                                        int64_t ld_out, int64_t units, const Columns<N, SMALL> &col, int64_t unit,
+                                        int64_t ch, int64_t i0, int64_t i1, int64_t b, int64_t s0, int64_t s1, bool head,
+                                        const Parts &part, int32_t &tail) {
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  int used = 0;
+  bool bad = false;
+  sum_tokens<N, SMALL>(c, E, ld, (int)max(s0, i0), (int)min(s1, i1), col, acc, used, bad);
+  if (bad)
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = __builtin_nanf("");
+  const bool more = s1 > i1 && i1 < c.T;
+  if (head || more) {
+    const int64_t p = ch * 2 + (head ? 0 : 1);
+    store_n<N>(part.sum + (p * units + unit) * N, N, acc);
+    if (unit == 0) part.used[p] = used;
+    if (!head) tail = (int32_t)b;
+  } else {
+    const float w = bag_weight(c, used);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] *= w;
+    col.store(out, out_type, b * ld_out, acc);
+  }
+  return more;
+}
+
 // One unit of one chunk of positions (see the top).  A bag belongs to the chunk that holds its start; an
 // empty one at the very end to the last chunk.
+// Bags of few tokens on the average (bag_blocks > 0): a chunk's thread would take many of them one after the other,
+// each with its own wait for its start, its tokens and its rows.  There a thread of the first bag_blocks blocks
+// takes one unit of one bag, if it has up to LONG_BAG positions; a chunk, which is no longer than that, is
+// left with the bags that cover its first or its last position and are longer.
+constexpr int64_t LONG_BAG = 128;
+
 template <int N, bool SMALL, class TE>
 __global__ void __launch_bounds__(EB) embed_bags_k(EmbedCall c, const TE *__restrict__ E, int64_t ld, void *out,
                                                    int32_t out_type, int64_t ld_out, int64_t units, int lg,
-                                                   int64_t chunks, Parts part) {
+                                                   int64_t chunks, int64_t bag_blocks, Parts part) {
   const int64_t L = 1ll << lg;
   int64_t ch, unit;
-  item_of(units, ch, unit);
+  int32_t tail = -1;
+  if ((int64_t)blockIdx.x < bag_blocks) {
+    item_of(blockIdx.x, units, ch, unit);
+    if (ch >= c.B) return;
+    const int64_t s0 = max<int64_t>(c.bags[ch], 0), s1 = min(c.bags[ch + 1], c.T);
+    if (s1 - s0 <= LONG_BAG)
+      sum_bag<N, SMALL>(c, E, ld, out, out_type, ld_out, units, Columns<N, SMALL>(unit, c.d), unit, 0, 0, c.T, ch, s0, s1,
+                        false, part, tail);
+    return;
+  }
+  item_of(blockIdx.x - bag_blocks, units, ch, unit);
   if (ch >= chunks) return;
   const Columns<N, SMALL> col(unit, c.d);
   const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
-  int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i0);
-  bool head = b > c.B || c.bags[b] != i0;
-  if (head) --b;
-  int32_t tail = -1;
-  for (; b >= 0 && b < c.B; ++b, head = false) {
-    const int64_t s0 = c.bags[b], s1 = c.bags[b + 1];
-    if (!head && s0 >= i1 && i1 < c.T) break;
-    const int64_t lo = max(s0, i0), hi = min(s1, i1);
-    float acc[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.f;
-    int used = 0;
-    bool bad = false;
-    sum_tokens<N, SMALL>(c, E, ld, (int)lo, (int)hi, col, acc, used, bad);
-    if (bad)
-#pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = __builtin_nanf("");
-    const bool more = s1 > i1 && i1 < c.T;
-    if (head || more) {
-      const int64_t p = ch * 2 + (head ? 0 : 1);
-      store_n<N>(part.sum + (p * units + unit) * N, N, acc);
-      if (unit == 0) part.used[p] = used;
-      if (!head) tail = (int32_t)b;
-    } else {
-      const float w = bag_weight(c, used);
-#pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] *= w;
-      col.store(out, out_type, b * ld_out, acc);
+  if (bag_blocks) {
+    const int64_t first = lower_bound<int64_t>(c.bags, c.B + 1, i0 + 1) - 1, last = lower_bound<int64_t>(c.bags, c.B + 1, i1) - 1;
+    for (int64_t b = first; b >= 0 && b < c.B; b = b == first ? last : -1) {
+      const int64_t s0 = max<int64_t>(c.bags[b], 0), s1 = min(c.bags[b + 1], c.T);
+      if (s1 - s0 > LONG_BAG)
+        sum_bag<N, SMALL>(c, E, ld, out, out_type, ld_out, units, col, unit, ch, i0, i1, b, s0, s1, s0 < i0, part, tail);
+      if (last == first) break;
     }
-    if (more) break;
+  } else {
+    int64_t b = lower_bound<int64_t>(c.bags, c.B + 1, i0);
+    bool head = b > c.B || c.bags[b] != i0;
+    if (head) --b;
+    for (; b >= 0 && b < c.B; ++b, head = false) {
+      const int64_t s0 = c.bags[b], s1 = c.bags[b + 1];
+      if (!head && s0 >= i1 && i1 < c.T) break;
+      if (sum_bag<N, SMALL>(c, E, ld, out, out_type, ld_out, units, col, unit, ch, i0, i1, b, s0, s1, head, part, tail)) break;
+    }
   }
   if (unit == 0) part.tail[ch] = tail;
 }
@@ -280,7 +314,7 @@ __global__ void __launch_bounds__(EB) embed_join_k(EmbedCall c, void *out, int32
   float acc[N];
   int used = 0;
   if ((int64_t)blockIdx.x < short_blocks) {
-    item_of(units, ch, unit);
+    item_of(blockIdx.x, units, ch, unit);
     if (ch >= chunks) return;
     b = part.tail[ch];
     if (b < 0) return;
@@ -633,7 +667,7 @@ __global__ void __launch_bounds__(EB) embed_runs_k(EmbedCall c, const uint32_t *
                                                    int64_t chunks, float *__restrict__ part) {
   const int64_t L = 1ll << lg;
   int64_t ch, unit;
-  item_of(units, ch, unit);
+  item_of(blockIdx.x, units, ch, unit);
   if (ch >= chunks) return;
   const Columns<N, SMALL> col(unit, c.d);
   const int64_t i0 = ch * L, i1 = min(c.T, i0 + L);
@@ -706,7 +740,7 @@ __global__ void __launch_bounds__(EB) embed_runs_join_k(EmbedCall c, const uint3
   uint32_t run;
   float acc[N];
   if ((int64_t)blockIdx.x < short_blocks) {
-    item_of(units, ch, unit);
+    item_of(blockIdx.x, units, ch, unit);
     const int64_t i0 = ch * L, i1 = i0 + L;
     if (ch >= chunks || i1 >= c.T) return;
     run = key[i1];
@@ -824,8 +858,12 @@ hipError_t launch_embed(const EmbedCall &c, const void *table, int32_t table_typ
     part.sum = aligned<float>(ws);
     part.used = reinterpret_cast<int32_t *>(part.sum + chunks * 2 * units * N);
     part.tail = part.used + 2 * chunks;
-    hipLaunchKernelGGL((embed_bags_k<N, SMALL, TE>), dim3((unsigned)shorts), dim3(EB), 0, s, c, E, ld_table, out, out_type,
-                       ld_out, units, lg, chunks, part);
+    // By bags up to 16 tokens a bag (us, both kernels; by bags, by chunks): 125 features in 16 bits, 56,837 tokens in
+    // 29,305 bags 20, 42; 240,000 in 30,000 30, 47; 480,000 54, 62; but 1,000,003 x 784 in 20,000 241, 211.
+    const int64_t bag_blocks = c.T <= 16 * c.B ? div_up(c.B * units, EB) : 0;
+    if (!grid_fits(bag_blocks + shorts)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((embed_bags_k<N, SMALL, TE>), dim3((unsigned)(bag_blocks + shorts)), dim3(EB), 0, s, c, E, ld_table, out,
+                       out_type, ld_out, units, lg, chunks, bag_blocks, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks == 1) return e;
     hipLaunchKernelGGL((embed_join_k<N, SMALL>), dim3((unsigned)all), dim3(EB), 0, s, c, out, out_type, ld_out, units, lg,
