@@ -255,10 +255,11 @@ GradTiles tile_plan(int64_t n, int64_t d, int64_t m) {
   }
   t.dc = round_up(d + 1, 4);
   t.fw = feature_blocks(d + 1);
-  const int64_t most = KERNEL_BYTES / (4 * t.svp) / ST * ST;
+  t.splits = 8;
+  // as many samples at a time as KERNEL_BYTES hold of their kernel values and of the shares' sums
+  const int64_t per = t.svp > t.splits * t.dc ? 4 * t.svp : 4 * t.splits * t.dc, most = KERNEL_BYTES / per / ST * ST;
   t.mc = round_up(m, ST);
   if (t.mc > most) t.mc = most < ST ? ST : most;
-  t.splits = 8;
   return t;
 }
 

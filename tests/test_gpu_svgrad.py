@@ -198,3 +198,48 @@ def test_binding_refusals():
             bad()
     with pytest.raises(svmx.SvmError):
         svmx.svm_objective_grad(X, y, a, -1.0)
+
+
+def test_more_samples_than_are_held_at_once():
+    """Few training rows, many samples, long rows: the samples are taken in several turns."""
+    n, d, m = 40, 1100, 70000
+    X, y, a = machine(n, d, 8)
+    gamma = 2.0 / d
+    g = torch.Generator().manual_seed(3)
+    base = torch.rand(500, d, generator=g)
+    Q = base.repeat(140, 1).cuda()  # the same samples in every turn
+    up = torch.ones(500, dtype=torch.float64)
+    ref, err = reference(X, a * y, gamma, base, up)
+    got = svmx.svm_predict_grad(X.cuda(), y.cuda(), a.cuda(), gamma, Q)
+    check(got[:500], ref, err)
+    assert torch.equal(got.view(140, 500, d)[3], got.view(140, 500, d)[0])
+    ends = [got[-500:], got[30000:30500]]
+    for e in ends:
+        check(e, ref, err)
+
+
+def test_huge_gamma_and_far_rows():
+    """Where gamma |x|^2 leaves fp32 every kernel value is 0 but those of equal rows, whose differences are 0."""
+    for d in (20, 200):
+        X, y, a = machine(300, d, 2)
+        for gamma in (1e30, 1e38):
+            got = svmx.svm_predict_grad((X * 1e6).cuda(), y.cuda(), a.cuda(), gamma, (X[:100] * 1e6).contiguous().cuda())
+            assert bool((got == 0).all())
+            assert bool((svmx.svm_objective_grad((X * 1e6).cuda(), y.cuda(), a.cuda(), gamma) == 0).all())
+
+
+def test_rows_whose_squares_overflow():
+    """A support vector or sample past fp32's squares has no neighbour; the others' gradients are as without it."""
+    for d, m in ((20, 5), (20, 100), (200, 100)):
+        X, y, a = machine(300, d, 3, share=1.0)
+        Q = X[:m].contiguous().clone()
+        clean = a.clone()
+        clean[7] = 0.0
+        want = svmx.svm_predict_grad(X.cuda(), y.cuda(), clean.cuda(), 0.1, Q.cuda())
+        X[7] = 1e25
+        got = svmx.svm_predict_grad(X.cuda(), y.cuda(), a.cuda(), 0.1, Q.cuda())
+        assert (got - want).abs().max() <= 1e-5 * want.abs().max()
+        Q[2] = 3e30
+        got = svmx.svm_predict_grad(X.cuda(), y.cuda(), a.cuda(), 0.1, Q.cuda())
+        assert bool((got[2] == 0).all())
+        assert bool(svmx.svm_objective_grad(X.cuda(), y.cuda(), a.cuda(), 0.1).isfinite().all())
