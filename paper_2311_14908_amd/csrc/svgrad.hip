@@ -211,7 +211,9 @@ inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 struct GradTiles {
   int32_t *sv_row;    // [n]
   float *coef;        // [n]: c_j (fp32)
-  int32_t *count;     // support vectors; [1]: bits of the largest row scale, [2]: exponent above every |c_j| x scale
+  int32_t *count;     // support vectors
+  int32_t *hist;      // [256]: support vectors by the exponent of their row scale, + 128
+  int32_t *info;      // what grad_transpose_k or grad_pack_k made of hist and cmax: MainRows, exponent above every |c_j|
   float *cmax;        // [COMPACT_MAX]: largest |c_j| of each workgroup of the compaction
   int32_t nblocks;    // of them
   SplitX sv, q;       // split rows (compact; q = sv for the objective's gradient)
@@ -277,7 +279,9 @@ int64_t tile_views(GradTiles &t, void *ws, int64_t n, int64_t d, int64_t m, bool
   };
   t.sv_row = static_cast<int32_t *>(take(4 * n));
   t.coef = static_cast<float *>(take(4 * n));
-  t.count = static_cast<int32_t *>(take(12));
+  t.count = static_cast<int32_t *>(take(4));
+  t.hist = static_cast<int32_t *>(take(4 * 256));
+  t.info = static_cast<int32_t *>(take(12));
   t.cmax = static_cast<float *>(take(4 * COMPACT_MAX));
   t.sv = split_views(take(gram_split_scratch_bytes(n, d)), n, d);
   t.q = objective ? t.sv : split_views(take(gram_split_scratch_bytes(m, d)), m, d);
@@ -299,6 +303,7 @@ __global__ void __launch_bounds__(CB) grad_compact_k(SvGradCall c, GradTiles t) 
   __shared__ int red[CB / 64];
   __shared__ float top[CB / 64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (blockIdx.x == 0 && threadIdx.x < 256) t.hist[threadIdx.x] = 0;
   const int64_t chunk = ((c.n + gridDim.x - 1) / gridDim.x + CB - 1) / CB * CB;
   const int64_t c0 = min(c.n, blockIdx.x * chunk), c1 = min(c.n, c0 + chunk);
   int before = 0;
@@ -343,40 +348,37 @@ __global__ void __launch_bounds__(CB) grad_compact_k(SvGradCall c, GradTiles t) 
   for (int q = 1; q < CB / 64; ++q) most = fmaxf(most, top[q]);
   t.cmax[blockIdx.x] = most;
   if (blockIdx.x == gridDim.x - 1) t.count[0] = base;
-  if (blockIdx.x == 0) {
-    t.count[1] = 0;
-    t.count[2] = -100000;
-  }
 }
 
-// Split rows of the support vectors (blocks up to sv_blocks) and of the samples; the largest scale of the
-// former, and the exponent of the largest |c_j| times the scale (maxima, so their order does not matter).
+// A row scale is 2^e; its place among the exponents.
+__device__ __forceinline__ int scale_bin(float scale) {
+  int e = 0;
+  (void)frexpf(scale, &e);
+  return min(max(e - 1 + 128, 0), 255);
+}
+
+// Rows of zeros have no magnitude (their scale is 1), rows whose norm overflows have no neighbour but their copies.
+__device__ __forceinline__ bool has_bin(float scale, float nrm) { return nrm < INFINITY && !(nrm == 0.f && scale == 1.f); }
+
+// Split rows of the support vectors (blocks up to sv_blocks) and of the samples; how many of the former have which
+// scale (whole numbers, so the order in which they are added does not matter).
 __global__ void __launch_bounds__(TB) grad_split_k(SplitRows sv, SplitRows q, int64_t d, GradTiles t, int32_t sv_blocks) {
   if ((int)blockIdx.x >= sv_blocks) {
     split_rows_block(q, d, blockIdx.x - sv_blocks, gridDim.x - sv_blocks, [](int64_t pos) { return pos; });
     return;
   }
+  __shared__ int hist[256];
+  hist[threadIdx.x] = 0;
+  __syncthreads();
   const int64_t nsv = t.count[0];
   sv.count = nsv;
   split_rows_block(sv, d, blockIdx.x, sv_blocks, [](int64_t pos) { return pos; });
   // this workgroup's own rows again: their scales, just written by lane 0 of each row group
   const int per = TB / sv.gs, g = threadIdx.x & (sv.gs - 1), mine = threadIdx.x / sv.gs;
-  int most[2] = {0, -100000};
   for (int64_t r = (int64_t)blockIdx.x * per + mine; g == 0 && r < nsv; r += (int64_t)sv_blocks * per)
-    if (sv.s.nrm[r] < INFINITY) {
-      int ec = 0, es = 0;
-      (void)frexpf(t.coef[r], &ec);
-      (void)frexpf(sv.s.scale[r], &es);
-      most[0] = max(most[0], __float_as_int(sv.s.scale[r]));
-      most[1] = max(most[1], ec + es);
-    }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) most[k] = max(most[k], __shfl_xor(most[k], o));
-    if ((threadIdx.x & 63) == 0 && most[k] > __atomic_load_n(&t.count[1 + k], __ATOMIC_RELAXED))
-      atomicMax(&t.count[1 + k], most[k]);
-  }
+    if (has_bin(sv.s.scale[r], sv.s.nrm[r])) atomicAdd(&hist[scale_bin(sv.s.scale[r])], 1);
+  __syncthreads();
+  if (hist[threadIdx.x]) atomicAdd(&t.hist[threadIdx.x], hist[threadIdx.x]);
 }
 
 __device__ __forceinline__ float wave_most(float v) {
@@ -393,6 +395,57 @@ __device__ __forceinline__ int coef_exp(const GradTiles &t) {
   return e;
 }
 
+// All rows of a product share one scale, the largest row's, and a value is good to 2^-39 of it.  So that a few rows
+// far larger than the others (an outlier, a marker for missing values) do not cost those their digits, rows more
+// than 2^16 times larger than the smallest tenth of them stay out of the tiles ("wide"), and grad_finish_k adds
+// them one by one.
+struct MainRows {
+  int bin;     // of the largest row in the tiles
+  bool wide;   // whether there are larger ones
+  __device__ __forceinline__ int exp() const { return bin - 128 + 1; }  // 2^exp is above every row in the tiles
+  __device__ __forceinline__ bool holds(float scale, float nrm) const { return nrm < INFINITY && (scale_bin(scale) <= bin || nrm == 0.f); }
+};
+
+__device__ __forceinline__ MainRows main_rows(const GradTiles &t) {
+  const int lane = threadIdx.x & 63;
+  const int4 h = *reinterpret_cast<const int4 *>(&t.hist[4 * lane]);
+  const int n[4] = {h.x, h.y, h.z, h.w};
+  int upto = h.x + h.y + h.z + h.w;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o);
+    if (lane >= o) upto += v;
+  }
+  const int total = __shfl(upto, 63);
+  int before = upto - (h.x + h.y + h.z + h.w), small = 256, top = -1, main = -1;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    before += n[q];
+    if (small == 256 && n[q] && 10LL * before >= total) small = 4 * lane + q;
+    if (n[q]) top = 4 * lane + q;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    small = min(small, __shfl_xor(small, o));
+    top = max(top, __shfl_xor(top, o));
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (n[q] && 4 * lane + q <= small + 16) main = 4 * lane + q;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) main = max(main, __shfl_xor(main, o));
+  return {main < 0 ? 128 : main, top > main};
+}
+
+// For the kernels that follow: once for all their waves.
+__device__ __forceinline__ void leave_info(const GradTiles &t, const MainRows &main, int ec) {
+  if (threadIdx.x != 0) return;
+  t.info[0] = main.bin;
+  t.info[1] = main.wide ? 1 : 0;
+  t.info[2] = ec;
+}
+__device__ __forceinline__ MainRows known_rows(const GradTiles &t) { return {t.info[0], t.info[1] != 0}; }
+
 // Tile i of `tiles`, so that each XCD (workgroup % 8) takes a contiguous share of them.
 __device__ __forceinline__ bool xcd_item(int64_t tiles, int64_t i, int64_t &item) {
   const int64_t share = (tiles + 7) / 8;
@@ -400,27 +453,40 @@ __device__ __forceinline__ bool xcd_item(int64_t tiles, int64_t i, int64_t &item
   return i / 8 < share && item < tiles;
 }
 
-// Rows by feature, c_j x_j at 2^X_EXP over the largest of all, and after the last feature c_j at 2^X_EXP over the
-// largest: 32 support vectors x 64 features a workgroup, through LDS; past the last support vector zeros.
+// Rows by feature, c_j x_j at 2^X_EXP over the largest c times the largest row, and after the last feature c_j at
+// 2^X_EXP over the largest: 32 support vectors x 64 features a workgroup, through LDS; past the last support vector, and
+// for rows that are not in the tiles, zeros.
 __global__ void __launch_bounds__(TB) grad_transpose_k(const float *__restrict__ X, int64_t d, GradTiles t) {
   __shared__ float v[32][65];
   const int nsv = t.count[0];
   const int s0 = blockIdx.x * 32;
-  if (s0 >= (nsv + ST - 1) / ST * ST) return;
+  if (s0 > 0 && s0 >= (nsv + ST - 1) / ST * ST) return;
   const int64_t f0 = (int64_t)blockIdx.y * 64;
   const int ec = coef_exp(t);
-  const int ex = t.count[2];
-  const double one = ldexp(1.0, X_EXP - ec), scale = ldexp(1.0, X_EXP - ex);
+  const MainRows rows = main_rows(t);
+  if (s0 == 0 && f0 == 0) leave_info(t, rows, ec);
+  if (nsv == 0) return;
+  __shared__ int32_t row[32];
+  __shared__ float coef[32];
+  if (threadIdx.x < 32) {
+    const int j = s0 + threadIdx.x;
+    const bool in = j < nsv && rows.holds(t.sv.scale[min(j, nsv - 1)], t.sv.nrm[min(j, nsv - 1)]);
+    row[threadIdx.x] = in ? t.sv_row[j] : -1;
+    coef[threadIdx.x] = in ? ldexpf(t.coef[j], X_EXP - ec) : 0.f;  // (powers of two: one rounding in all)
+  }
+  __syncthreads();
+  const int es = rows.exp(), mine = threadIdx.x % 64;
+  const int64_t at = f0 + mine;
+  float x[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const int r = threadIdx.x / 64 + 4 * k, f = threadIdx.x % 64;
-    float x = 0.f;
-    // (a row whose norm overflows has no neighbour but its copies, which add nothing)
-    if (s0 + r < nsv && f0 + f <= d && t.sv.nrm[s0 + r] < INFINITY) {
-      const double c = (double)t.coef[s0 + r];
-      x = (float)(f0 + f < d ? (double)X[(int64_t)t.sv_row[s0 + r] * d + f0 + f] * (c * scale) : c * one);
-    }
-    v[r][f] = x;
+    const int r = row[threadIdx.x / 64 + 4 * k];
+    x[k] = r >= 0 && at < d ? X[(int64_t)r * d + at] : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float c = coef[threadIdx.x / 64 + 4 * k];
+    v[threadIdx.x / 64 + 4 * k][mine] = at < d ? ldexpf(x[k], -es) * c : at == d ? c : 0.f;
   }
   __syncthreads();
   // thread: 8 support vectors of one feature
@@ -700,9 +766,8 @@ __global__ void __launch_bounds__(PB, 1) grad_product_k(SvGradCall c, GradTiles 
 //   [feature chunk of 32][support vector][hi 32 | lo 32]   the rows, 16-byte pieces permuted by ^ (row % 8)
 //   [feature][hi 32 | lo 32]                               the same by feature, pieces permuted likewise
 //   [2][32] floats: -gamma log2(e) |x|^2, c_j 2^W_EXP / 2^ec
-// All rows have one scale, 2^X_EXP over the largest row's, so that no factor is left for each pair: a value is within
-// 2^-39 of the largest of all before it is multiplied, 2^-24 of rows up to 2^15 times smaller.  Where the features
-// leave room in their last block of 16, one more "feature" of ones turns the sum of the weights into a
+// All rows have one scale, 2^X_EXP over the largest row's in the tiles (main_rows), so that no factor is left for
+// each pair.  Where the features leave room in their last block of 16, one more "feature" of ones turns the sum of the weights into a
 // column of the second product.
 __device__ __forceinline__ int sv_slot(int j) {  // support vector at place j of an operand
   return (j & 4) ? 16 + 4 * (j >> 3) + (j & 3) : 4 * (j >> 3) + (j & 3);
@@ -710,16 +775,18 @@ __device__ __forceinline__ int sv_slot(int j) {  // support vector at place j of
 
 __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, float cexp) {
   const int nsv = t.count[0], s0 = blockIdx.x * 32, nk = (t.fb + 1) / 2;
-  if (s0 >= nsv) return;
+  if (s0 > 0 && s0 >= nsv) return;
   char *img = t.image + blockIdx.x * image_bytes(t.fb);
   const int ec = coef_exp(t);
-  int es = 0;
-  (void)frexpf(__int_as_float(t.count[1]), &es);
-  const float scale = ldexpf(1.0f, X_EXP - es);
+  const MainRows main = main_rows(t);
+  if (s0 == 0) leave_info(t, main, ec);
+  if (nsv == 0) return;
+  const float scale = ldexpf(1.0f, X_EXP - main.exp());
+  const auto holds = [&](int j) { return j < nsv && main.holds(t.sv.scale[j], t.sv.nrm[j]); };
   for (int p = threadIdx.x; p < nk * 128; p += TB) {  // a piece of the rows, hi and lo
     const int k = p >> 7, row = (p >> 2) & 31, g = p & 3, f0 = k * 32 + g * 8;
     split_h8 h, l;
-    const bool in = s0 + row < nsv && t.sv.nrm[min(s0 + row, nsv - 1)] < INFINITY;
+    const bool in = holds(s0 + row);
     const float *x = c.X + (int64_t)(in ? t.sv_row[s0 + row] : 0) * c.d;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -740,7 +807,7 @@ __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, flo
     for (int e = 0; e < 8; ++e) {
       const int j = s0 + sv_slot(8 * g + e);
       float x = f == c.d ? (float)(1 << X_EXP) : 0.f;
-      if (j < nsv && f < c.d && t.sv.nrm[j] < INFINITY) x = c.X[(int64_t)t.sv_row[j] * c.d + f] * scale;
+      if (f < c.d && holds(j)) x = c.X[(int64_t)t.sv_row[j] * c.d + f] * scale;
       h[e] = (_Float16)x;
       l[e] = (_Float16)(x - (float)h[e]);
     }
@@ -750,7 +817,7 @@ __global__ void __launch_bounds__(TB) grad_pack_k(SvGradCall c, GradTiles t, flo
   img += t.fb * 2048;
   if (threadIdx.x < 32) {
     const int j = s0 + threadIdx.x;
-    const bool in = j < nsv && t.sv.nrm[j] < INFINITY;  // (an infinite norm: only copies of the row are near it)
+    const bool in = holds(j);
     float *o = reinterpret_cast<float *>(img) + threadIdx.x;
     o[0] = in ? cexp * t.sv.nrm[j] : 0.f;
     o[32] = in ? ldexpf(t.coef[j], W_EXP - ec) : 0.f;
@@ -786,8 +853,7 @@ __global__ void __launch_bounds__(TB, FB <= 4 ? 3 : 2) grad_short_k(SvGradCall c
   const int stages = (nsv + 31) / 32, per = (stages + t.splits - 1) / t.splits;
   const int st0 = min(stages, split * per), st1 = min(stages, st0 + per);
   const int64_t qw = q0 + w * 16 * QB;  // this wave's samples
-  int es = 0;
-  (void)frexpf(__int_as_float(t.count[1]), &es);
+  const int es = known_rows(t).exp();
   h8 qh[QB][NK], ql[QB][NK];
   float sb[QB], nb[QB], sum[QB];
   v4f acc[QB][FB];
@@ -929,23 +995,22 @@ __global__ void __launch_bounds__(TB, FB <= 4 ? 3 : 2) grad_short_k(SvGradCall c
   leave(st1 - st0 > FOLD);
 }
 
-// One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x).
-__global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, int64_t q_first, int64_t q_end) {
+// One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x), and the wide rows one by one, as the pass
+// does it.
+__global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, double cexp, int64_t q_first, int64_t q_end) {
   const bool objective = c.Q == nullptr;
   const int nsv = t.count[0], lane = threadIdx.x & 63;
   if (objective) q_end = min(q_end, (int64_t)nsv);
   const int64_t l = (int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6), q = q_first + l;
   if (q >= q_end) return;
-  const int ec = coef_exp(t);
-  const int ex = t.count[2];
-  int es = 0;
-  (void)frexpf(__int_as_float(t.count[1]), &es);
+  const int ec = t.info[2];
+  const MainRows main = known_rows(t);
   const int64_t row = objective ? t.sv_row[q] : q;
   const double up = objective ? -(double)t.coef[q] : c.up ? c.up[q] : 1.0;
   const double f = nsv ? 2.0 * c.gamma * up : 0.0;
-  // powers of two that the sums and the weights' sum were scaled by: c_j / 2^ec and x_j / 2^es each, or c_j x_j / 2^ex
+  // powers of two that the sums and the weights' sum were scaled by
   const bool ones = !t.fb || c.d % 16;
-  const double scale = ldexp(1.0, (t.fb ? ec + es : ex) - W_EXP - X_EXP);
+  const double scale = ldexp(1.0, ec + main.exp() - W_EXP - X_EXP);
   const double sscale = ldexp(1.0, ec - W_EXP - (ones ? X_EXP : 0));
   const int splits = !nsv ? 0 : t.fb ? t.splits : product_shares(t, c.d + 1, q_end - q_first, nsv);
   float s = 0.f;
@@ -954,6 +1019,7 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   const double sum = sscale * (double)s;
   const float *x = (objective ? c.X : c.Q) + row * c.d;
+  float *out = c.out + row * c.d;
   for (int64_t at = 4 * lane; at < c.d; at += 256) {
     float xv[4], o[4] = {};
     load_n<4>(x + at, c.d - at, xv);
@@ -965,7 +1031,35 @@ __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, i
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - sum * (double)xv[e]));
-    store_n<4>(c.out + row * c.d + at, c.d - at, o);
+    store_n<4>(out + at, c.d - at, o);
+  }
+  for (int j0 = 0; main.wide && j0 < nsv; j0 += 64) {
+    const int mine = min(j0 + lane, nsv - 1);
+    const float sc = t.sv.scale[mine], nrm = t.sv.nrm[mine];
+    unsigned long long wide = __ballot(j0 + lane < nsv && has_bin(sc, nrm) && !main.holds(sc, nrm));
+    for (; wide; wide &= wide - 1) {
+      const int j = j0 + __builtin_ctzll(wide);
+      if (objective && j == q) continue;
+      const float *xj = c.X + (int64_t)t.sv_row[j] * c.d;
+      double d2 = 0.0;
+      for (int64_t k = lane; k < c.d; k += 64) {
+        const double v = (double)(xj[k] - x[k]);
+        d2 = __builtin_fma(v, v, d2);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) d2 += __shfl_xor(d2, o);
+      const double wt = f * (double)t.coef[j] * rbf_of_d2(cexp, d2);
+      if (wt == 0.0) continue;
+      for (int64_t at = 4 * lane; at < c.d; at += 256) {  // (this lane's own part of the row)
+        float o[4], xv[4], v[4];
+        load_n<4>(out + at, c.d - at, o);
+        load_n<4>(x + at, c.d - at, xv);
+        load_n<4>(xj + at, c.d - at, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (float)((double)o[e] + wt * (double)(v[e] - xv[e]));
+        store_n<4>(out + at, c.d - at, o);
+      }
+    }
   }
 }
 
@@ -1004,7 +1098,8 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
       case 7: go(grad_short_k<7, true>, grad_short_k<7, false>); break;
       default: go(grad_short_k<8, true>, grad_short_k<8, false>);
     }
-    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, (int64_t)0, c.m);
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, -c.gamma * 1.4426950408889634,
+                       (int64_t)0, c.m);
     return hipGetLastError();
   }
   if (c.d / 64 + 1 > 65535) return hipErrorInvalidValue;
@@ -1026,7 +1121,8 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
       hipLaunchKernelGGL(grad_product_k<4>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
     else
       hipLaunchKernelGGL(grad_product_k<5>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
-    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t, q0, q1);
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t,
+                       -c.gamma * 1.4426950408889634, q0, q1);
   }
   return hipGetLastError();
 }

@@ -243,3 +243,38 @@ def test_rows_whose_squares_overflow():
         got = svmx.svm_predict_grad(X.cuda(), y.cuda(), a.cuda(), 0.1, Q.cuda())
         assert bool((got[2] == 0).all())
         assert bool(svmx.svm_objective_grad(X.cuda(), y.cuda(), a.cuda(), 0.1).isfinite().all())
+
+
+@pytest.mark.parametrize("d,m", [(20, 150), (64, 40), (200, 150)])
+@pytest.mark.parametrize("share,factor", [(0.01, 1e12), (0.3, 1e9), (0.7, 1e9), (0.02, 3e5), (0.5, 1e-8), (0.03, 1e17)])
+def test_rows_of_very_different_sizes(d, m, share, factor):
+    """Outliers and markers: a share of the rows (and of the samples) is larger or smaller than the others by `factor`;
+    gamma suits the ordinary rows.  Their gradients keep the tolerance they would have alone."""
+    n = 400
+    X, y, a = machine(n, d, 11)
+    g = torch.Generator().manual_seed(5)
+    Q = torch.rand(m, d, generator=g)
+    Q[:20] = X[:20]
+    big = torch.rand(n, generator=g) < share
+    X[big] *= factor
+    Q[20:30] = X[big][:10].repeat(10, 1)[:10]  # samples that are such rows
+    Q[30:40] *= factor
+    gamma = 2.0 / d
+    up = torch.randn(m, generator=g, dtype=torch.float64)
+    ref, err = reference(X, a * y, gamma, Q, up)
+    args = [t.cuda() for t in (X, y, a)]
+    check(svmx.svm_predict_grad(*args, gamma, Q.cuda(), up.cuda()), ref, err)
+    c = a * y
+    ref, err = reference(X, c, gamma, X, -c, own=torch.arange(n))
+    check(svmx.svm_objective_grad(*args, gamma), ref, err)
+
+
+def test_rows_of_zeros():
+    for d in (20, 200):
+        X, y, a = machine(300, d, 4)
+        X *= 1e-9
+        X[torch.arange(300) % 3 == 0] = 0.0
+        gamma = 2e18 / d
+        c = a * y
+        ref, err = reference(X, c, gamma, X, -c, own=torch.arange(300))
+        check(svmx.svm_objective_grad(X.cuda(), y.cuda(), a.cuda(), gamma), ref, err)
