@@ -995,69 +995,79 @@ __global__ void __launch_bounds__(TB, FB <= 4 ? 3 : 2) grad_short_k(SvGradCall c
   leave(st1 - st0 > FOLD);
 }
 
-// One wave a sample: out = u 2 gamma (the shares' sums - (sum c K) x), and the wide rows one by one, as the pass
-// does it.
-__global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, double cexp, int64_t q_first, int64_t q_end) {
+// out = u 2 gamma (the shares' sums - (sum c K) x): gs lanes of a wave a sample (a power of two that covers its units of
+// four features, at most 64).  Then the wide rows one by one, as the pass does it, a wave a sample.
+__global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, double cexp, int gs, int64_t q_first, int64_t q_end) {
   const bool objective = c.Q == nullptr;
-  const int nsv = t.count[0], lane = threadIdx.x & 63;
+  const int nsv = t.count[0], lane = threadIdx.x & 63, g = lane & (gs - 1);
   if (objective) q_end = min(q_end, (int64_t)nsv);
-  const int64_t l = (int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6), q = q_first + l;
-  if (q >= q_end) return;
+  const int64_t l0 = ((int64_t)blockIdx.x * (TB / 64) + (threadIdx.x >> 6)) * (64 / gs);  // the wave's first sample
+  if (q_first + l0 >= q_end) return;
   const int ec = t.info[2];
   const MainRows main = known_rows(t);
-  const int64_t row = objective ? t.sv_row[q] : q;
-  const double up = objective ? -(double)t.coef[q] : c.up ? c.up[q] : 1.0;
-  const double f = nsv ? 2.0 * c.gamma * up : 0.0;
+  const auto row_of = [&](int64_t q) { return objective ? (int64_t)t.sv_row[q] : q; };
+  const auto factor_of = [&](int64_t q) {
+    const double up = objective ? -(double)t.coef[q] : c.up ? c.up[q] : 1.0;
+    return nsv ? 2.0 * c.gamma * up : 0.0;
+  };
   // powers of two that the sums and the weights' sum were scaled by
   const bool ones = !t.fb || c.d % 16;
   const double scale = ldexp(1.0, ec + main.exp() - W_EXP - X_EXP);
   const double sscale = ldexp(1.0, ec - W_EXP - (ones ? X_EXP : 0));
   const int splits = !nsv ? 0 : t.fb ? t.splits : product_shares(t, c.d + 1, q_end - q_first, nsv);
-  float s = 0.f;
-  for (int k = lane; k < splits; k += 64) s += ones ? t.part[(k * t.mc + l) * t.dc + c.d] : t.sums[k * t.mc + l];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  const double sum = sscale * (double)s;
-  const float *x = (objective ? c.X : c.Q) + row * c.d;
-  float *out = c.out + row * c.d;
-  for (int64_t at = 4 * lane; at < c.d; at += 256) {
-    float xv[4], o[4] = {};
-    load_n<4>(x + at, c.d - at, xv);
+  const float *X = objective ? c.X : c.Q;
+  {
+    const int64_t l = l0 + lane / gs, q = min(q_first + l, q_end - 1), row = row_of(q);
+    float s = 0.f;
+    for (int k = g; k < splits; k += gs) s += ones ? t.part[(k * t.mc + (q - q_first)) * t.dc + c.d] : t.sums[k * t.mc + (q - q_first)];
+    for (int o = gs >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    const double sum = sscale * (double)s, f = factor_of(q);
+    for (int64_t at = 4 * g; at < c.d && q_first + l < q_end; at += 4 * gs) {
+      float xv[4], o[4] = {};
+      load_n<4>(X + row * c.d + at, c.d - at, xv);
 #pragma unroll 8
-    for (int k = 0; k < splits; ++k) {
-      const v4f v = *reinterpret_cast<const v4f *>(&t.part[((int64_t)k * t.mc + l) * t.dc + at]);
+      for (int k = 0; k < splits; ++k) {
+        const v4f v = *reinterpret_cast<const v4f *>(&t.part[((int64_t)k * t.mc + l) * t.dc + at]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += v[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - sum * (double)xv[e]));
-    store_n<4>(out + at, c.d - at, o);
-  }
-  for (int j0 = 0; main.wide && j0 < nsv; j0 += 64) {
-    const int mine = min(j0 + lane, nsv - 1);
-    const float sc = t.sv.scale[mine], nrm = t.sv.nrm[mine];
-    unsigned long long wide = __ballot(j0 + lane < nsv && has_bin(sc, nrm) && !main.holds(sc, nrm));
-    for (; wide; wide &= wide - 1) {
-      const int j = j0 + __builtin_ctzll(wide);
-      if (objective && j == q) continue;
-      const float *xj = c.X + (int64_t)t.sv_row[j] * c.d;
-      double d2 = 0.0;
-      for (int64_t k = lane; k < c.d; k += 64) {
-        const double v = (double)(xj[k] - x[k]);
-        d2 = __builtin_fma(v, v, d2);
+        for (int e = 0; e < 4; ++e) o[e] += v[e];
       }
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) d2 += __shfl_xor(d2, o);
-      const double wt = f * (double)t.coef[j] * rbf_of_d2(cexp, d2);
-      if (wt == 0.0) continue;
-      for (int64_t at = 4 * lane; at < c.d; at += 256) {  // (this lane's own part of the row)
-        float o[4], xv[4], v[4];
-        load_n<4>(out + at, c.d - at, o);
-        load_n<4>(x + at, c.d - at, xv);
-        load_n<4>(xj + at, c.d - at, v);
+      for (int e = 0; e < 4; ++e) o[e] = (float)(f * (scale * (double)o[e] - sum * (double)xv[e]));
+      store_n<4>(c.out + row * c.d + at, c.d - at, o);
+    }
+  }
+  if (!main.wide) return;
+  __threadfence_block();  // other lanes of the wave read these rows again
+  for (int64_t q = q_first + l0; q < min(q_end, q_first + l0 + 64 / gs); ++q) {
+    const double f = factor_of(q);
+    const float *x = X + row_of(q) * c.d;
+    float *out = c.out + row_of(q) * c.d;
+    for (int j0 = 0; j0 < nsv; j0 += 64) {
+      const int mine = min(j0 + lane, nsv - 1);
+      const float sc = t.sv.scale[mine], nrm = t.sv.nrm[mine];
+      unsigned long long wide = __ballot(j0 + lane < nsv && has_bin(sc, nrm) && !main.holds(sc, nrm));
+      for (; wide; wide &= wide - 1) {
+        const int j = j0 + __builtin_ctzll(wide);
+        if (objective && j == q) continue;
+        const float *xj = c.X + (int64_t)t.sv_row[j] * c.d;
+        double d2 = 0.0;
+        for (int64_t k = lane; k < c.d; k += 64) {
+          const double v = (double)(xj[k] - x[k]);
+          d2 = __builtin_fma(v, v, d2);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (float)((double)o[e] + wt * (double)(v[e] - xv[e]));
-        store_n<4>(out + at, c.d - at, o);
+        for (int o = 32; o > 0; o >>= 1) d2 += __shfl_xor(d2, o);
+        const double wt = f * (double)t.coef[j] * rbf_of_d2(cexp, d2);
+        if (wt == 0.0) continue;
+        for (int64_t at = 4 * lane; at < c.d; at += 256) {  // (the same lane's part of the row each time)
+          float o[4], xv[4], v[4];
+          load_n<4>(out + at, c.d - at, o);
+          load_n<4>(x + at, c.d - at, xv);
+          load_n<4>(xj + at, c.d - at, v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = (float)((double)o[e] + wt * (double)(v[e] - xv[e]));
+          store_n<4>(out + at, c.d - at, o);
+        }
       }
     }
   }
@@ -1081,6 +1091,8 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
   const int64_t svb = split_rows_blocks(sv), qb = split_rows_blocks(q);
   hipLaunchKernelGGL(grad_split_k, dim3((unsigned)(svb + qb)), dim3(TB), 0, s, sv, q, c.d, t, (int32_t)svb);
   const float cexp = (float)(-c.gamma * 1.4426950408889634);
+  int gs = 1;
+  while (gs < 64 && 4LL * gs < c.d) gs <<= 1;
   if (objective) hipLaunchKernelGGL(grad_zero_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c);
   if (t.fb) {
     hipLaunchKernelGGL(grad_pack_k, dim3((unsigned)(t.svp / 32)), dim3(TB), 0, s, c, t, cexp);
@@ -1098,8 +1110,8 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
       case 7: go(grad_short_k<7, true>, grad_short_k<7, false>); break;
       default: go(grad_short_k<8, true>, grad_short_k<8, false>);
     }
-    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / 64)), dim3(TB), 0, s, c, t, -c.gamma * 1.4426950408889634,
-                       (int64_t)0, c.m);
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(c.m, TB / gs)), dim3(TB), 0, s, c, t, -c.gamma * 1.4426950408889634,
+                       gs, (int64_t)0, c.m);
     return hipGetLastError();
   }
   if (c.d / 64 + 1 > 65535) return hipErrorInvalidValue;
@@ -1121,8 +1133,8 @@ hipError_t launch_tiles(const SvGradCall &c, void *ws, hipStream_t s) {
       hipLaunchKernelGGL(grad_product_k<4>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
     else
       hipLaunchKernelGGL(grad_product_k<5>, dim3((unsigned)pb), dim3(PB), 0, s, c, t, q0, q1);
-    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / 64)), dim3(TB), 0, s, c, t,
-                       -c.gamma * 1.4426950408889634, q0, q1);
+    hipLaunchKernelGGL(grad_finish_k, dim3((unsigned)div_up(q1 - q0, TB / gs)), dim3(TB), 0, s, c, t,
+                       -c.gamma * 1.4426950408889634, gs, q0, q1);
   }
   return hipGetLastError();
 }
