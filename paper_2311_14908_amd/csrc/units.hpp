@@ -35,6 +35,16 @@ __device__ __forceinline__ Raw<N, T> load_whole(const T *__restrict__ p) {
   return r;
 }
 
+// N values that nothing else on this card reads soon: they take no room in the caches.
+template <int N, class T>
+__device__ __forceinline__ Raw<N, T> load_once(const T *__restrict__ p) {
+  Raw<N, T> r;
+#pragma unroll
+  for (int q = 0; q < N / Raw<N, T>::M; ++q)
+    r.v[q] = __builtin_nontemporal_load(reinterpret_cast<const typename VecOf<T, Raw<N, T>::M>::type *>(p + q * Raw<N, T>::M));
+  return r;
+}
+
 // Of which `left` are in the row; the others come as 0.
 template <int N, class T>
 __device__ __forceinline__ Raw<N, T> load_raw(const T *__restrict__ p, int64_t left) {
@@ -78,6 +88,19 @@ __device__ __forceinline__ void store_n(T *__restrict__ p, int64_t left, const f
 #pragma unroll
     for (int e = 0; e < N; ++e)
       if (e < left) p[e] = (T)v[e];
+  }
+}
+
+// N values, all of them in the row, that nothing reads soon.
+template <int N, class T>
+__device__ __forceinline__ void store_once(T *__restrict__ p, const float (&v)[N]) {
+  constexpr int M = N < UNIT<T> ? N : UNIT<T>;
+#pragma unroll
+  for (int q = 0; q < N; q += M) {
+    typename VecOf<T, M>::type u;
+#pragma unroll
+    for (int e = 0; e < M; ++e) u[e] = (T)v[q + e];
+    __builtin_nontemporal_store(u, reinterpret_cast<typename VecOf<T, M>::type *>(p + q));
   }
 }
 

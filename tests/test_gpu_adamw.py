@@ -260,3 +260,38 @@ def test_binding_refusals():
     with pytest.raises(svmx.SvmError):
         svmx.svm_adamw(p, g, m, v, 0, 1e-3)
     svmx.svm_adamw([], [], [], [], 1, 1e-3)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-15, 1e-8, 1.0, 1e25])
+@pytest.mark.parametrize("dtype", [F32, F8])
+def test_any_eps(eps, dtype):
+    """Tiny second moments with an eps that does or does not hide them: below it the step is as exact."""
+    sizes = [2048, 5000]
+    g = torch.Generator().manual_seed(9)
+    p = [torch.randn(s, generator=g) * 1e-3 for s in sizes]
+    gr = [torch.randn(s, generator=g) * torch.exp(torch.randn(s, generator=g) * 3 - 20) for s in sizes]
+    pd, gd = cuda((p, gr))
+    md, vd, ms, vs = svmx.svm_adamw_states(pd, dtype)
+    svmx.svm_adamw(pd, gd, md, vd, 1, 1e-3, eps=eps, m_scale=ms, v_scale=vs)
+    for i in range(len(sizes)):
+        zero = torch.zeros(sizes[i])
+        p1, m1, v1, ep, _, _ = step64(p[i], gr[i], zero, zero, 1, 1e-3, 0.0, 1.0, 0.9, 0.999, eps)
+        # v is held in fp32: what is denormal there has an error of half the smallest number
+        vmin = 2.0 ** -149
+        moved = 1e-3 * gr[i].double().abs() / (torch.sqrt(((v1 - vmin).clamp_min(0)) / 1e-3) + eps) - 1e-3 * gr[i].double().abs() / (
+            torch.sqrt(v1 / 1e-3) + eps)
+        within(pd[i], p1, ep + moved.nan_to_num(nan=1.0, posinf=1.0))
+
+
+def test_blocks_at_every_place_step_alike():
+    """A value's step does not depend on where in its tensor it stands, in whole chunks or behind them."""
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(256, generator=g)
+    for dtype in (F32, F8):
+        p = [x.repeat(21).cuda()]
+        gr = [(x.flip(0) * 0.1).repeat(21).cuda()]
+        m, v, ms, vs = svmx.svm_adamw_states(p, dtype)
+        for t in range(1, 4):
+            svmx.svm_adamw(p, gr, m, v, t, 1e-2, m_scale=ms, v_scale=vs)
+        rows = p[0].view(21, 256)
+        assert torch.equal(rows, rows[:1].expand_as(rows))
