@@ -9,7 +9,14 @@
 // The weight's and bias's gradients: a workgroup walks rows and keeps dy h and dy of its columns in
 // registers, leaves one partial row, and a second kernel adds those in their order (no atomics, so results
 // repeat bit for bit; a launch of one workgroup writes them itself).
-// Rows longer than a workgroup holds are read again from the caches for every sum.
+// Rows longer than 2,048 units are read again from the caches for every sum.
+//
+// Measured on an MI355X, where a copy of a large tensor runs at 4.8 TB/s (what fits 256 MB, in its last-level cache,
+// faster).  norm_k: 20,000 x 784 fp32 22 us, 5.7 TB/s; 65,536 x 4,096 bf16 208 us, 5.2; 30,000 x 4,096 fp32
+// 183 us, 5.4.  norm_grad_k: 60,001 x 301 fp32 38 us, and 6 for the sums, 4.9 TB/s; 65,536 x 4,096 bf16 327 us and
+// 8, 4.8; 40,000 x 8,000 bf16 432 us, 4.4; 12,000 x 8,000 fp32 218 us, 5.2.  What costs: 16-bit rows at odd
+// pitches, whose 16-byte loads straddle lines (16,000 x 12,001 326 us, 2.4 TB/s), and the long rows' second reading
+// (4,000 x 20,001 fp32, forward 222 us, 2.9 TB/s; gradient 400 us, 2.4).
 #include "layers.hpp"
 #include "units.hpp"
 
@@ -19,34 +26,39 @@ namespace svmx {
 
 namespace {
 
-constexpr int NB = 256;  // threads of a workgroup
-constexpr int NW = NB / 64;
+constexpr int NB = 256;  // threads of a workgroup, where a row does not take a larger one
 
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a row of `units` units is spread: g lanes (NB: the workgroup), k units a lane; k = 0: too long.
+// How a row of `units` units is spread: g lanes of a workgroup of t threads, k units a lane; k = 0: too long.
 struct RowShape {
-  int g, k;
+  int g, k, t;
 };
 
+// As many waves as keep K at 2 (the gradient's 16-bit sums take 50 registers a unit): 30,000 x 4,096 fp32 takes the
+// gradient 272 us with 512 threads and 306 with 256 and K = 4; 12,000 x 8,000 218 with 1,024, 469 as a long row.  One
+// unit a lane and twice the threads is slower forwards (60,000 x 2,000 267 us, not 193): half its lanes idle.
 RowShape row_shape(int64_t units) {
   if (units <= 64) {
     int g = 1;
     while (g < units) g <<= 1;
-    return {g, 1};
+    return {g, 1, NB};
   }
-  if (units <= 256) return {64, units <= 128 ? 2 : 4};
-  if (units <= 4 * NB) return {NB, units <= 2 * NB ? 2 : 4};
-  return {NB, 0};
+  if (units <= 256) return {64, units <= 128 ? 2 : 4, NB};
+  if (units <= 2 * NB) return {NB, 2, NB};
+  if (units <= 1024) return {512, 2, 512};
+  if (units <= 2048) return {1024, 2, 1024};
+  return {NB, 0, NB};
 }
 
-// Sums of a and b over the g lanes of a row (all of them get it); g = NB: over the workgroup.
+// Sums of a and b over the g lanes of a row (all of them get it); g = T: over the workgroup.
+template <int T>
 __device__ __forceinline__ void row_sums(float &a, float &b, int g, float (*lds)[2]) {
   for (int o = (g < 64 ? g : 64) >> 1; o > 0; o >>= 1) {
     a += __shfl_xor(a, o);
     b += __shfl_xor(b, o);
   }
-  if (g == NB) {
+  if (g == T) {
     if ((threadIdx.x & 63) == 0) {
       lds[threadIdx.x >> 6][0] = a;
       lds[threadIdx.x >> 6][1] = b;
@@ -54,7 +66,7 @@ __device__ __forceinline__ void row_sums(float &a, float &b, int g, float (*lds)
     __syncthreads();
     a = b = 0.f;
 #pragma unroll
-    for (int q = 0; q < NW; ++q) {
+    for (int q = 0; q < T / 64; ++q) {
       a += lds[q][0];
       b += lds[q][1];
     }
@@ -70,13 +82,13 @@ __device__ __forceinline__ void load_weight(const void *w, int32_t type, int64_t
 }
 
 // Rows of g lanes, K units a lane; every workgroup walks rows.
-template <int K, class TX, class TY>
-__global__ void __launch_bounds__(NB) norm_k(NormCall c, int g, float eps, TY *__restrict__ y, int64_t ld_y,
-                                             float *__restrict__ mean, float *__restrict__ rstd) {
+template <int K, int T, class TX, class TY>
+__global__ void __launch_bounds__(T) norm_k(NormCall c, int g, float eps, TY *__restrict__ y, int64_t ld_y,
+                                            float *__restrict__ mean, float *__restrict__ rstd) {
   constexpr int N = UNIT<TX>;
-  __shared__ float lds[NW][2];
+  __shared__ float lds[T / 64][2];
   const TX *X = static_cast<const TX *>(c.x);
-  const int per = NB / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
+  const int per = T / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
   float w[K][N], b[K][N];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -89,18 +101,23 @@ __global__ void __launch_bounds__(NB) norm_k(NormCall c, int g, float eps, TY *_
     const int64_t r = r0 + grp;
     const bool in = r < c.n;
     const TX *x = X + (in ? r : c.n - 1) * c.ld_x;
+    Raw<N, TX> xv[K];
     float v[K][N];
     float s = 0.f, none = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int64_t at = (int64_t)(lane + k * g) * N;
-      load_n<N>(x + at, c.d - at, v[k]);
+      xv[k] = load_raw<N>(x + at, c.d - at);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
+      for (int e = 0; e < N; ++e) v[k][e] = xv[k].at(e);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
       for (int e = 0; e < N; ++e) s += v[k][e];
-    row_sums(s, none, g, lds);
+    row_sums<T>(s, none, g, lds);
     const float mu = s / fd;
     float q = 0.f;
 #pragma unroll
@@ -112,7 +129,7 @@ __global__ void __launch_bounds__(NB) norm_k(NormCall c, int g, float eps, TY *_
         if (e < left) q = __builtin_fmaf(v[k][e], v[k][e], q);
       }
     }
-    row_sums(q, none, g, lds);
+    row_sums<T>(q, none, g, lds);
     const float rs = 1.0f / __builtin_sqrtf(q / fd + eps);
     if (!in) continue;
 #pragma unroll
@@ -130,12 +147,12 @@ __global__ void __launch_bounds__(NB) norm_k(NormCall c, int g, float eps, TY *_
   }
 }
 
-// Rows longer than 4 NB units: a workgroup a row, three passes.
+// Rows longer than 2,048 units: a workgroup a row, three passes.
 template <class TX, class TY>
 __global__ void __launch_bounds__(NB) norm_long_k(NormCall c, float eps, TY *__restrict__ y, int64_t ld_y,
                                                   float *__restrict__ mean, float *__restrict__ rstd) {
   constexpr int N = UNIT<TX>;
-  __shared__ float lds[NW][2];
+  __shared__ float lds[NB / 64][2];
   const int64_t units = (c.d + N - 1) / N;
   const float fd = (float)c.d;
   for (int64_t r = blockIdx.x; r < c.n; r += gridDim.x) {
@@ -147,7 +164,7 @@ __global__ void __launch_bounds__(NB) norm_long_k(NormCall c, float eps, TY *__r
 #pragma unroll
       for (int e = 0; e < N; ++e) s += v[e];
     }
-    row_sums(s, none, NB, lds);
+    row_sums<NB>(s, none, NB, lds);
     const float mu = s / fd;
     for (int64_t u = threadIdx.x; u < units; u += NB) {
       float v[N];
@@ -156,7 +173,7 @@ __global__ void __launch_bounds__(NB) norm_long_k(NormCall c, float eps, TY *__r
       for (int e = 0; e < N; ++e)
         if (e < c.d - u * N) q = __builtin_fmaf(v[e] - mu, v[e] - mu, q);
     }
-    row_sums(q, none, NB, lds);
+    row_sums<NB>(q, none, NB, lds);
     const float rs = 1.0f / __builtin_sqrtf(q / fd + eps);
     for (int64_t u = threadIdx.x; u < units; u += NB) {
       float v[N], w[N], b[N];
@@ -202,15 +219,16 @@ __device__ __forceinline__ void leave_sum(const NormCall &c, const float *lds, i
 }
 
 // The gradient, rows as in norm_k.  TY: type of dy (dx has x's).
-template <int K, class TX, class TY>
-__global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g) {
+// (512 threads: 128 registers at most, so that two workgroups share a CU; 40,000 x 8,000 bf16 572 -> 442 us.)
+template <int K, int T, class TX, class TY>
+__global__ void __launch_bounds__(T, T == 512 ? 4 : 1) norm_grad_k(NormCall c, NormGrad p, int g) {
   constexpr int N = UNIT<TX>;
   extern __shared__ float cols[];  // [rows side by side][dp], in one go for dw and one for db
-  __shared__ float lds[NW][2];
+  __shared__ float lds[T / 64][2];
   const TX *X = static_cast<const TX *>(c.x);
   const TY *DY = static_cast<const TY *>(p.dy);
   TX *DX = static_cast<TX *>(p.dx);
-  const int per = NB / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
+  const int per = T / g, lane = threadIdx.x & (g - 1), grp = threadIdx.x / g;
   float w[K][N], dw[K][N], db[K][N];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -225,11 +243,13 @@ __global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g)
     const bool in = r < c.n;
     const int64_t rr = in ? r : c.n - 1;
     float h[K][N], t[K][N];
+    Raw<N, TX> hv[K];
+    Raw<N, TY> tv[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int64_t at = (int64_t)(lane + k * g) * N;
-      load_n<N>(X + rr * c.ld_x + at, c.d - at, h[k]);
-      load_n<N>(DY + rr * p.ld_dy + at, c.d - at, t[k]);
+      hv[k] = load_raw<N>(X + rr * c.ld_x + at, c.d - at);
+      tv[k] = load_raw<N>(DY + rr * p.ld_dy + at, c.d - at);
     }
     const float mu = p.mean[rr], rs = p.rstd[rr];
     float s1 = 0.f, s2 = 0.f;
@@ -237,7 +257,8 @@ __global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g)
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        h[k][e] = (h[k][e] - mu) * rs;  // (past the row's end dy is 0)
+        h[k][e] = (hv[k].at(e) - mu) * rs;  // (past the row's end dy is 0)
+        t[k][e] = tv[k].at(e);
         const float q = t[k][e] * w[k][e];
         s1 += q;
         s2 = __builtin_fmaf(q, h[k][e], s2);
@@ -247,7 +268,7 @@ __global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g)
         }
         t[k][e] = q;
       }
-    row_sums(s1, s2, g, lds);
+    row_sums<T>(s1, s2, g, lds);
     s1 /= fd;
     s2 /= fd;
     if (!in) continue;
@@ -261,17 +282,31 @@ __global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g)
   }
   if (!p.dw && !p.db) return;
   float *part = p.part + (int64_t)blockIdx.x * 2 * p.dp;
-  for (int pass = 0; pass < 2; ++pass) {
-    __syncthreads();
+  if constexpr (T > NB) {  // one row: its lanes hold the sums of the workgroup
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int64_t at = (int64_t)(lane + k * g) * N;
-      if (at < p.dp)
-#pragma unroll
-        for (int e = 0; e < N; ++e) cols[grp * p.dp + at + e] = pass == 0 ? dw[k][e] : db[k][e];
+      if (gridDim.x > 1) {
+        store_n<N>(part + at, p.dp - at, dw[k]);
+        store_n<N>(part + p.dp + at, p.dp - at, db[k]);
+      } else {
+        if (p.dw) store_any<N>(p.dw, c.w_type, at, c.d - at, dw[k]);
+        if (p.db) store_any<N>(p.db, c.w_type, at, c.d - at, db[k]);
+      }
     }
-    __syncthreads();
-    leave_sum<N>(c, cols, per, p.dp, part + pass * p.dp, pass == 0 ? p.dw : p.db);
+  } else {
+    for (int pass = 0; pass < 2; ++pass) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int64_t at = (int64_t)(lane + k * g) * N;
+        if (at < p.dp)
+#pragma unroll
+          for (int e = 0; e < N; ++e) cols[grp * p.dp + at + e] = pass == 0 ? dw[k][e] : db[k][e];
+      }
+      __syncthreads();
+      leave_sum<N>(c, cols, per, p.dp, part + pass * p.dp, pass == 0 ? p.dw : p.db);
+    }
   }
 }
 
@@ -279,7 +314,7 @@ __global__ void __launch_bounds__(NB) norm_grad_k(NormCall c, NormGrad p, int g)
 template <class TX, class TY>
 __global__ void __launch_bounds__(NB) norm_grad_long_k(NormCall c, NormGrad p) {
   constexpr int N = UNIT<TX>;
-  __shared__ float lds[NW][2];
+  __shared__ float lds[NB / 64][2];
   const int64_t units = (c.d + N - 1) / N;
   const float fd = (float)c.d;
   for (int64_t r = blockIdx.x; r < c.n; r += gridDim.x) {
@@ -308,7 +343,7 @@ __global__ void __launch_bounds__(NB) norm_grad_long_k(NormCall c, NormGrad p) {
         if (pass == 1) store_n<N>(static_cast<TX *>(p.dx) + r * p.ld_dx + u * N, left, t);
       }
       if (pass == 0) {
-        row_sums(s1, s2, NB, lds);
+        row_sums<NB>(s1, s2, NB, lds);
         s1 /= fd;
         s2 /= fd;
       }
@@ -371,11 +406,11 @@ __global__ void __launch_bounds__(NB) norm_grad_sum_k(NormCall c, NormGrad p, in
   store_any<4>(out, c.w_type, at, c.d - at, s);
 }
 
-// Workgroups that walk rows: each row group takes 8 rows or more, 4 workgroups a CU at most (what their
-// partial rows cost, against what one more wave hides).
-int64_t grad_blocks(int64_t n, int g) {
-  const int64_t want = div_up(n, 8 * (NB / g));
-  return want > 1024 ? 1024 : want < 1 ? 1 : want;
+// Workgroups that walk rows: each row group takes 8 rows or more, 16 waves a CU at most (what their partial rows
+// cost, against what one more wave hides: 60,001 x 301 takes 44 us, and 50 with twice as many).
+int64_t grad_blocks(int64_t n, const RowShape &sh) {
+  const int64_t want = div_up(n, 8 * (sh.t / sh.g)), most = 1024 * NB / sh.t;
+  return want > most ? most : want < 1 ? 1 : want;
 }
 int64_t cols_blocks(int64_t n) { return n > 64 * 16 ? 64 : div_up(n, 16); }
 
@@ -403,16 +438,20 @@ hipError_t launch_layernorm(const NormCall &c, float eps, void *y, int32_t y_typ
     using TX = std::remove_pointer_t<decltype(tx)>;
     using TY = std::remove_pointer_t<decltype(ty)>;
     const RowShape sh = row_shape(div_up(c.d, UNIT<TX>));
-    const int64_t want = div_up(c.n, NB / sh.g), blocks = want > 4096 ? 4096 : want;
+    const int64_t want = div_up(c.n, sh.t / sh.g), blocks = want > 4096 ? 4096 : want;
     const auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(NB), 0, s, c, sh.g, eps, static_cast<TY *>(y), ld_y, mean, rstd);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3((unsigned)sh.t), 0, s, c, sh.g, eps, static_cast<TY *>(y), ld_y, mean, rstd);
     };
-    if (sh.k == 1)
-      go(norm_k<1, TX, TY>);
+    if (sh.t == 1024)
+      go(norm_k<2, 1024, TX, TY>);
+    else if (sh.t == 512)
+      go(norm_k<2, 512, TX, TY>);
+    else if (sh.k == 1)
+      go(norm_k<1, NB, TX, TY>);
     else if (sh.k == 2)
-      go(norm_k<2, TX, TY>);
+      go(norm_k<2, NB, TX, TY>);
     else if (sh.k == 4)
-      go(norm_k<4, TX, TY>);
+      go(norm_k<4, NB, TX, TY>);
     else
       hipLaunchKernelGGL((norm_long_k<TX, TY>), dim3((unsigned)blocks), dim3(NB), 0, s, c, eps, static_cast<TY *>(y), ld_y,
                          mean, rstd);
@@ -423,7 +462,7 @@ hipError_t launch_layernorm(const NormCall &c, float eps, void *y, int32_t y_typ
 int64_t layernorm_grad_scratch_bytes(int64_t n, int64_t d, int32_t x_type) {
   const int64_t units = div_up(d, unit_of(x_type));
   const RowShape sh = row_shape(units);
-  const int64_t rows = sh.k ? grad_blocks(n, sh.g) : cols_blocks(n);
+  const int64_t rows = sh.k ? grad_blocks(n, sh) : cols_blocks(n);
   return 8 * rows * units * unit_of(x_type) + 256;
 }
 
@@ -440,17 +479,21 @@ hipError_t launch_layernorm_grad(const NormCall &c, const void *dy, int32_t dy_t
     const RowShape sh = row_shape(units);
     int64_t rows = 0;  // partial rows
     if (c.n > 0 && sh.k) {
-      rows = grad_blocks(c.n, sh.g);
-      const size_t lds = dw || db ? (size_t)(NB / sh.g) * p.dp * 4 : 0;
+      rows = grad_blocks(c.n, sh);
+      const size_t lds = (dw || db) && sh.t == NB ? (size_t)(sh.t / sh.g) * p.dp * 4 : 0;
       const auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(NB), lds, s, c, p, sh.g);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3((unsigned)sh.t), lds, s, c, p, sh.g);
       };
-      if (sh.k == 1)
-        go(norm_grad_k<1, TX, TY>);
+      if (sh.t == 1024)
+        go(norm_grad_k<2, 1024, TX, TY>);
+      else if (sh.t == 512)
+        go(norm_grad_k<2, 512, TX, TY>);
+      else if (sh.k == 1)
+        go(norm_grad_k<1, NB, TX, TY>);
       else if (sh.k == 2)
-        go(norm_grad_k<2, TX, TY>);
+        go(norm_grad_k<2, NB, TX, TY>);
       else
-        go(norm_grad_k<4, TX, TY>);
+        go(norm_grad_k<4, NB, TX, TY>);
       if (rows == 1) return hipGetLastError();
     } else if (c.n > 0) {
       hipLaunchKernelGGL((norm_grad_long_k<TX, TY>), dim3((unsigned)(c.n > 4096 ? 4096 : c.n)), dim3(NB), 0, s, c, p);
