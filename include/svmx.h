@@ -405,7 +405,7 @@ typedef struct {
  * scales too).  e4m3 states: every block of 256 values is kept over its largest magnitude / 448, to
  * nearest even, a second moment above 0 never as 0; a block below 2^-100 becomes zeros; a value that is
  * not finite is kept as NaN and leaves its block's scale alone (the square of a finite gradient that
- * overflows is kept as the largest fp32).  One launch for every 40 tensors.
+ * overflows is kept as the largest fp32).  One launch for every 40 tensors of the same types.
  * EINVAL: NULL pointers, unknown types, negative counts, step < 1, betas outside [0, 1), lr, eps, weight
  * decay or grad_scale that are negative or not finite.
  */

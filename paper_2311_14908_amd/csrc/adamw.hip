@@ -4,7 +4,7 @@
 // p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // Every value is read and written once, so the step is bound by memory (28 bytes a parameter with 32-bit
 // states and fp32 parameters, 16 with 8-bit states).  The list travels in the kernel's arguments, 40 tensors
-// a launch: no table in device memory, no copy, nothing to wait for, and a captured launch holds all it
+// a launch (of one type of state, of gradient and of what is updated): no table in device memory, no copy, nothing to wait for, and a captured launch holds all it
 // needs.  A workgroup takes CHUNK values of one tensor; it finds the tensor by bisecting the first chunk
 // of each.
 //
