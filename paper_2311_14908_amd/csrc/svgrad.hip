@@ -16,7 +16,7 @@
 // to 2^-14, and a kernel value of 2^-18 still has all its 22 that way.
 //
 // Measured on an MI355X (a large fp16 product of the library: 1,295 TFLOP/s):
-//   one sample against 20,000 x 784, 15,000 support vectors   14.4 us + 4.9 the join; 47 MB, 3.3 TB/s
+//   one sample against 20,000 x 784, 15,000 support vectors   13.1 us + 4.8 the join; 47 MB, 3.6 TB/s
 //   objective, 20,000 x 784, 15,000 support vectors           1,670 us: products 899 (1,197 TFLOP/s of fp16 work), kernel
 //       values 590 (the symmetric half: 912), the end 92, split rows 51, rows by feature 23, compact 9, zeros 6
 //   objective, 99,999 x 31, 30,000 support vectors            465 us: both products and the exponentials 445
@@ -35,12 +35,12 @@ namespace {
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int GB = 256, GU = 4;  // threads, units of four features a lane holds of a row
-constexpr int GL = 256;          // training rows looked at in one go
+constexpr int GL = GB;           // training rows looked at in one go
 constexpr int64_t FEW_D = 4LL * GU * 64;  // features the pass takes
 
 // Samples the pass takes: it costs about as much for every four, the tiles cost their preparation first.  Us a call
-// (pass, tiles), 60% support vectors: 16 samples against 20,000 x 784 91, 188; 32 166, 189; 64 316, 190; 32
-// against 300,000 x 64 189, 349; against 100,000 x 31 16 93, 124, but 32 176, 125.
+// (pass, tiles), 60% support vectors: 16 samples against 20,000 x 784 80, 188; 32 147, 189, and 4.5 for each
+// more; 32 against 300,000 x 64 189, 349; against 100,000 x 31 16 93, 124, but 32 176, 125.
 constexpr int64_t few_most(int64_t d) { return d >= 64 ? 32 : 16; }
 
 // Chunks of training rows: 32 rows each, at most 512 of them.
@@ -49,13 +49,43 @@ int64_t few_chunks(int64_t n) {
   return c > 512 ? 512 : c;
 }
 
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(b >> 32), CTRL, 0xF, 0xF, false);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)b, CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+
+// Sums over groups of gs lanes, to all of them.  Whole waves: inside rows of 16 lanes by DPP (neighbours, pairs, then
+// mirrored halves), a third of a shuffle's wait (15,000 x 784, one sample, 14.6 -> 13.1 us).
+template <bool WAVE, int M>
+__device__ __forceinline__ void group_sums(double (&s)[M], int gs) {
+  if (WAVE) {
+#pragma unroll
+    for (int q = 0; q < M; ++q) {
+      s[q] += from_lane<0xB1>(s[q]);
+      s[q] += from_lane<0x4E>(s[q]);
+      s[q] += from_lane<0x141>(s[q]);
+      s[q] += from_lane<0x140>(s[q]);
+      s[q] += __shfl_xor(s[q], 16);
+      s[q] += __shfl_xor(s[q], 32);
+    }
+    return;
+  }
+  for (int o = gs >> 1; o > 0; o >>= 1)
+#pragma unroll
+    for (int q = 0; q < M; ++q) s[q] += __shfl_xor(s[q], o);
+}
+
 // Workgroup (x, y): chunk x of the training rows, samples MQ y ..  The chunk's support vectors are listed in LDS;
 // gs lanes of a wave take one after the other and hold its row (the next one is on its way), the samples and
 // the sums: the squared differences are added in fp64, then c K (x_j - x_q) is added where it stands, so a
 // row is read once.  The differences are exact or nearly so, and nothing cancels afterwards.  Bound by memory and, in a
-// workgroup's last rows, latency: 15,000 of 20,000 rows of 784 features for one sample 14.4 us, 3.3 TB/s.
-template <int MQ>
-__global__ void __launch_bounds__(GB) sv_grad_few_k(SvGradCall c, double cexp, int gs, int64_t per, int64_t dc,
+// workgroup's last rows, latency: 15,000 of 20,000 rows of 784 features for one sample 13.1 us, 3.6 TB/s.  (Two waves
+// a SIMD: without the bound four samples take 258 registers and a half of the waves.)
+template <int MQ, bool WAVE>
+__global__ void __launch_bounds__(GB, 2) sv_grad_few_k(SvGradCall c, double cexp, int gs, int64_t per, int64_t dc,
                                                     float *__restrict__ part) {
   __shared__ int32_t rows[GL];
   __shared__ double coefs[GL];
@@ -122,9 +152,7 @@ __global__ void __launch_bounds__(GB) sv_grad_few_k(SvGradCall c, double cexp, i
             s[q] = __builtin_fma(f, f, s[q]);
           }
       }
-      for (int o = gs >> 1; o > 0; o >>= 1)
-#pragma unroll
-        for (int q = 0; q < MQ; ++q) s[q] += __shfl_xor(s[q], o);
+      group_sums<WAVE>(s, gs);
 #pragma unroll
       for (int q = 0; q < MQ; ++q) {
         const float wt = objective && q0 + q == rows[r] ? 0.f : (float)(coefs[r] * rbf_of_d2(cexp, s[q]));
@@ -197,10 +225,11 @@ hipError_t launch_few(const SvGradCall &c, void *ws, hipStream_t s) {
   const size_t lds = (size_t)(GB / gs) * dc * 4;
   const double cexp = -c.gamma * 1.4426950408889634;
   const dim3 grid((unsigned)chunks, (unsigned)(c.m == 1 ? 1 : div_up(c.m, 4)));
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(GB), lds, s, c, cexp, gs, per, dc, part); };
   if (c.m == 1)
-    hipLaunchKernelGGL(sv_grad_few_k<1>, grid, dim3(GB), lds, s, c, cexp, gs, per, dc, part);
+    gs == 64 ? go(sv_grad_few_k<1, true>) : go(sv_grad_few_k<1, false>);
   else
-    hipLaunchKernelGGL(sv_grad_few_k<4>, grid, dim3(GB), lds, s, c, cexp, gs, per, dc, part);
+    gs == 64 ? go(sv_grad_few_k<4, true>) : go(sv_grad_few_k<4, false>);
   hipLaunchKernelGGL(sv_grad_few_join_k, dim3((unsigned)div_up(dc, 64), (unsigned)c.m), dim3(GB), 0, s, c, chunks, dc, part);
   return hipGetLastError();
 }
