@@ -17,7 +17,7 @@
 //
 // Measured on an MI355X (a large fp16 product of the library: 1,295 TFLOP/s):
 //   one sample against 20,000 x 784, 15,000 support vectors   13.1 us + 4.8 the join; 47 MB, 3.6 TB/s
-//   objective, 20,000 x 784, 15,000 support vectors           1,670 us: products 899 (1,197 TFLOP/s of fp16 work), kernel
+//   objective, 20,000 x 784, 15,000 support vectors           1,620 us: products 850 (1,265 TFLOP/s of fp16 work), kernel
 //       values 590 (the symmetric half: 912), the end 92, split rows 51, rows by feature 23, compact 9, zeros 6
 //   objective, 99,999 x 31, 30,000 support vectors            465 us: both products and the exponentials 445
 //       (188 TFLOP/s: the exponentials and the splitting of their values keep the vector unit busy, not the matrix cores)
@@ -685,9 +685,10 @@ __device__ __forceinline__ int product_shares(const GradTiles &t, int64_t featur
 // 32 FW features x 256 samples of the second product, over one share of the support vectors; eight waves, each 16 FW
 // features x 64 samples.  Features are the row operand: a lane holds 4 consecutive ones of a sample.  A stage's
 // rows stand in LDS as in split_tile.hpp.  Three stages are in LDS: while one is multiplied the next one has
-// landed by half time (the only barrier of a stage), its feature operands are read during the second half, and
-// the one after is on its way.  15,000 x 15,000 values times 785 features 899 us, 1,197 TFLOP/s of fp16 work: 92% of the
-// library's large product; half the cycles of a wave are waits for its operands, LDS has no conflicts.
+// landed by half time (the only barrier of a stage), its features and half of its samples are read during the
+// second half, and the one after is on its way.  15,000 x 15,000 values times 785 features 850 us, 1,265 TFLOP/s of fp16 work, 98% of the
+// library's large product (900 and 1,195 in a row of such calls, at the clocks they leave).  LDS is read 80% of the time
+// (144 KB a stage for 1,920 cycles of products), without conflicts.
 constexpr int PB = 512;
 
 template <int FW>
@@ -738,11 +739,20 @@ __global__ void __launch_bounds__(PB, 1) grad_product_k(SvGradCall c, GradTiles 
       l[a] = S[buf][(wm * FW + a) * 128 + pl];
     }
   };
+  h8 bh[4], bl[4];
+  const auto samples = [&](int buf, int b) {
+    bh[b] = S[buf][(2 * FW + wn * 4 + b) * 128 + ph];
+    bl[b] = S[buf][(2 * FW + wn * 4 + b) * 128 + pl];
+  };
   int buf = 0;  // this stage's
   if (st0 < st1) load(0);
   landed();
   if (st0 + 1 < st1) load(1);
-  if (st0 < st1) features(0, ah, al);
+  if (st0 < st1) {
+    features(0, ah, al);
+    samples(0, 0);
+    samples(0, 1);
+  }
   // A sum over 15,000 support vectors is 1,400 roundings of a growing fp32 one after the other; cut every FOLD
   // stages it is a tenth of that, and the rest happens once a cut (the tile of sums stays in L2 between).
   int64_t st = st0;
@@ -755,20 +765,24 @@ __global__ void __launch_bounds__(PB, 1) grad_product_k(SvGradCall c, GradTiles 
     const int64_t cut = min(st1, st + FOLD);
     for (int64_t i = st; i < cut; ++i) {
       const auto multiply = [&](int b) {
-        const h8 bh = S[buf][(2 * FW + wn * 4 + b) * 128 + ph], bl = S[buf][(2 * FW + wn * 4 + b) * 128 + pl];
 #pragma unroll
-        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bh, acc[a][b], 0, 0, 0);
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bh[b], acc[a][b], 0, 0, 0);
 #pragma unroll
-        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bl, acc[a][b], 0, 0, 0);
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[a], bl[b], acc[a][b], 0, 0, 0);
 #pragma unroll
-        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[a], bh, acc[a][b], 0, 0, 0);
+        for (int a = 0; a < FW; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[a], bh[b], acc[a][b], 0, 0, 0);
       };
       const int next = buf == 2 ? 0 : buf + 1, after = next == 2 ? 0 : next + 1;
+      samples(buf, 2);
+      samples(buf, 3);
       multiply(0);
       multiply(1);
+      __builtin_amdgcn_sched_barrier(0);  // (the products would be moved behind the wait, and the load have half its time)
       landed();  // the next stage; everyone is done with the stage before this one
       if (i + 2 < st1) load(after);
       h8 nh[FW], nl[FW];
+      samples(next, 0);
+      samples(next, 1);
       features(next, nh, nl);  // (past the last stage: what the buffer holds, not used)
       multiply(2);
       multiply(3);
@@ -1037,7 +1051,8 @@ __global__ void __launch_bounds__(TB, FB <= 4 ? 3 : 2) grad_short_k(SvGradCall c
 }
 
 // out = u 2 gamma (the shares' sums - (sum c K) x): gs lanes of a wave a sample (a power of two that covers its units of
-// four features, at most 64).  Bound by memory: 20,000 x 784 and three shares 92 us, 99,999 x 31 9.  Then the wide rows one by one, as the pass does it, a wave a sample.
+// four features, at most 64).  Bound by memory: 15,000 x 784 and six shares 92 us, 4.1 TB/s; 99,999 x 31 9 us.  Then the
+// wide rows one by one, as the pass does it, a wave a sample.
 __global__ void __launch_bounds__(TB) grad_finish_k(SvGradCall c, GradTiles t, double cexp, int gs, int64_t q_first, int64_t q_end) {
   const bool objective = c.Q == nullptr;
   const int nsv = t.count[0], lane = threadIdx.x & 63, g = lane & (gs - 1);
