@@ -16,8 +16,8 @@
 //                                                   (the table is 103 MB)
 //   200,000 tokens of 512 fp32, no bags             148 us, 410 MB read and 410 MB written, 5.5 TB/s
 //   gradient, 5,000 tokens of 64 fp32, 2,000 rows   25 us: ranks 11, sums 10, join 4
-//   gradient, 1,000,003 tokens of 256 bf16, 65,537 rows  215 us: sums 135 (583 MB, 4.3 TB/s; rows are read in the
-//                                                   order of their tokens), sort 66, join 14
+//   gradient, 1,000,003 tokens of 256 bf16, 65,537 rows  212 us: sums 135 (583 MB, 4.3 TB/s; rows are read in the
+//                                                   order of their tokens), sort 62, join 14
 #include "layers.hpp"
 #include "units.hpp"
 
@@ -602,22 +602,27 @@ __global__ void __launch_bounds__(SC) radix_scan_k(uint32_t *__restrict__ hist, 
   if (w == 0) total[blockIdx.x * 64 + lane] = all;
 }
 
-// Every position of this block to its place: the positions with a smaller digit, those with its digit in
-// blocks before, and those before it in this block, 512 of them at a time (a wave counts its own by
-// ballots over the digit's bits).  A million positions 17.6 us a pass: 24 MB, bound by the chain of eight ballots and
-// the counts of eight waves that each turn of 512 positions waits for, not by memory.
+// Every position of this block to its place: the positions with a smaller digit, those with its digit in blocks
+// before, and those before it in this block.  Each wave takes an eighth of the block and counts its digits first, so that
+// every wave knows where each digit of its share starts and walks it without waiting for the others, PT times 64
+// positions on their way: the lanes of a digit are ranked by ballots over its bits, and their first one moves the digit's
+// place.  A million positions of 65,537 tokens 12 us the first pass and 20 the second, whose 4-byte stores go everywhere
+// (with barriers for every 512 positions of a block, 15 and 20); of 100 tokens 13 (17).
+constexpr int PT = 4;
+
 __global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__ key, const uint32_t *__restrict__ src,
                                                     uint32_t *__restrict__ key_out, uint32_t *__restrict__ src_out,
                                                     int64_t T, int shift, int bits, int64_t per,
                                                     const uint32_t *__restrict__ hist, const uint32_t *__restrict__ total) {
-  __shared__ uint32_t base[SB];  // next place of each digit
-  __shared__ uint32_t wave_n[SB / 64][SB];
+  __shared__ uint32_t next[SB / 64][SB];  // of each wave: next place of each digit
   __shared__ uint32_t wsum[SB / 64];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t dmask = (1u << bits) - 1u;
-  const int64_t i0 = blockIdx.x * per, i1 = min(T, i0 + per);
-  uint32_t nk = i0 + t < i1 ? key[i0 + t] : 0, ns = i0 + t < i1 ? src[i0 + t] : 0;  // the next ones, on their way
+  const int64_t share = per / (SB / 64);  // (a multiple of 64)
+  const int64_t i0 = min(T, blockIdx.x * per + w * share), i1 = min(min(T, (int64_t)(blockIdx.x + 1) * per), i0 + share);
   const uint32_t all = t <= (int)dmask ? total[t] : 0, before = hist[((int64_t)blockIdx.x << DIGIT_MAX) + t];
+#pragma unroll
+  for (int q = 0; q < SB / 64; ++q) next[q][t] = 0;
   uint32_t incl = all;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -626,47 +631,62 @@ __global__ void __launch_bounds__(SB) radix_place_k(const uint32_t *__restrict__
   }
   if (lane == 63) wsum[w] = incl;
   __syncthreads();
-  uint32_t b0 = incl - all + before;
-  for (int q = 0; q < w; ++q) b0 += wsum[q];
-  base[t] = b0;
+  for (int64_t r = i0 + lane; r < i1; r += 64 * PT) {
+    uint32_t k[PT];
 #pragma unroll
-  for (int q = 0; q < SB / 64; ++q) wave_n[q][t] = 0;
+    for (int q = 0; q < PT; ++q) k[q] = key[min(r + 64 * q, i1 - 1)];
+#pragma unroll
+    for (int q = 0; q < PT; ++q)
+      if (r + 64 * q < i1) atomicAdd(&next[w][(k[q] >> shift) & dmask], 1u);
+  }
+  uint32_t at = incl - all + before;
+  for (int q = 0; q < w; ++q) at += wsum[q];
   __syncthreads();
-  for (int64_t r = i0; r < i1; r += SB) {
-    const int64_t i = r + t;
-    const bool in = i < i1;
-    const uint32_t k = nk, s = ns, dig = (k >> shift) & dmask;
-    nk = i + SB < i1 ? key[i + SB] : 0;
-    ns = i + SB < i1 ? src[i + SB] : 0;
-    unsigned long long same = __ballot(in);
 #pragma unroll
-    for (int bit = 0; bit < DIGIT_MAX; ++bit) {
-      const unsigned long long m = __ballot(in && ((dig >> bit) & 1));
-      same &= (dig >> bit) & 1 ? m : ~m;
-    }
-    const uint32_t mine = __popcll(same & ((1ull << lane) - 1ull));
-    if (in && mine == 0) wave_n[w][dig] = __popcll(same);
-    __syncthreads();
-    // the counts of the waves become the places where each of them starts; the thread of a digit sees to it
-    uint32_t at = base[t];
+  for (int q = 0; q < SB / 64; ++q) {  // counts become places; the thread of a digit sees to it
+    const uint32_t n = next[q][t];
+    next[q][t] = at;
+    at += n;
+  }
+  __syncthreads();
+  uint32_t nk[PT], ns[PT];
+  const auto fetch = [&](int64_t r) {
 #pragma unroll
-    for (int q = 0; q < SB / 64; ++q) {
-      const uint32_t n = wave_n[q][t];
-      wave_n[q][t] = at;
-      at += n;
+    for (int q = 0; q < PT; ++q) {
+      const int64_t i = min(r + 64 * q + lane, i1 - 1);
+      nk[q] = key[i];
+      ns[q] = src[i];
     }
-    base[t] = at;
-    __syncthreads();
-    uint32_t to = 0;
-    if (in) to = wave_n[w][dig] + mine;
-    __syncthreads();
+  };
+  if (i0 < i1) fetch(i0);
+  for (int64_t r = i0; r < i1; r += 64 * PT) {
+    uint32_t k[PT], s[PT];
 #pragma unroll
-    for (int q = 0; q < SB / 64; ++q) wave_n[q][t] = 0;
-    if (in) {
-      key_out[to] = k;
-      src_out[to] = s;
+    for (int q = 0; q < PT; ++q) {
+      k[q] = nk[q];
+      s[q] = ns[q];
     }
-    __syncthreads();
+    if (r + 64 * PT < i1) fetch(r + 64 * PT);
+#pragma unroll
+    for (int q = 0; q < PT; ++q) {
+      const bool in = r + 64 * q + lane < i1;
+      const uint32_t dig = (k[q] >> shift) & dmask;
+      unsigned long long same = __ballot(in);
+#pragma unroll
+      for (int bit = 0; bit < DIGIT_MAX; ++bit) {
+        const unsigned long long m = __ballot((dig >> bit) & 1);
+        same &= (dig >> bit) & 1 ? m : ~m;
+      }
+      const uint32_t mine = __popcll(same & ((1ull << lane) - 1ull));
+      const uint32_t first = next[w][dig];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // every lane has read its digit's place
+      if (in && mine == 0) next[w][dig] = first + (uint32_t)__popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // and sees it moved
+      if (in) {
+        key_out[first + mine] = k[q];
+        src_out[first + mine] = s[q];
+      }
+    }
   }
 }
 
