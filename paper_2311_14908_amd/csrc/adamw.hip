@@ -11,8 +11,8 @@
 // Measured on an MI355X: 195 million parameters with 8-bit states and bf16 gradients, 2,730 MB, 460 us or
 // 5.9 TB/s; 102 million with fp32 states, 2,867 MB, 469 us or 6.1 TB/s (a copy of a large tensor: 4.8).  What
 // is read and written passes the caches by (non-temporal: 518 us and 524 without), and all loads of a wave
-// precede its arithmetic.  128 thousand parameters: 4 us, the call 10.  Of 146 tensors the largest is what
-// counts; of 146 small ones the caller's checks take longer than the four launches.
+// precede its arithmetic.  128 thousand parameters: 4 us, the call 6.  146
+// tensors of 100 values take the host 27 us, checks and four launches.
 //
 // 8-bit states: blocks of 256 values (one wave, 4 a lane), a code each in e4m3 (v_cvt_pk_fp8_f32, to nearest
 // even) and a scale in fp32, the block's largest magnitude / 448, so the largest value is exact and the

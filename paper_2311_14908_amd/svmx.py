@@ -400,7 +400,6 @@ def ovo_offsets(label: np.ndarray, k: int):
 
 _FLOATS = {torch.float32: SVM_F32, torch.bfloat16: SVM_BF16, torch.float16: SVM_F16}
 _TOKENS = {torch.int32: 4, torch.int64: 8}
-_STATES = {torch.float32: SVM_F32, torch.float8_e4m3fn: SVM_F8}
 _tls = threading.local()
 
 
@@ -620,18 +619,15 @@ def svm_adamw_states(params, dtype=torch.float32):
     return m, v, scales, [torch.zeros_like(s) for s in scales]
 
 
-def _flat(t, types, count, device, name):
-    """Address of a contiguous tensor of one of the types."""
-    if t.get_device() != device:
-        raise TypeError(f"{name} must be on the current device")
-    if t.dtype not in types or not t.is_contiguous():
-        raise TypeError(f"{name} must be contiguous and one of {[str(k) for k in types]} (got {t.dtype})")
-    if t.numel() != count:
-        raise ValueError(f"{name} must have {count} values (got {t.numel()})")
-    return t.data_ptr()
-
-
-_F32_ONLY = {torch.float32: SVM_F32}
+def _describe(*lists) -> bytes:
+    """The C array of svm_adamw_tensor for lists of tensors, checked (csrc/tensor_list.cpp)."""
+    global _describe
+    try:
+        from ._tensor_list import describe
+    except ImportError as e:
+        raise RuntimeError("_tensor_list.so is missing: build it with paper_2311_14908_amd.build.build()") from e
+    _describe = describe
+    return describe(*lists)
 
 
 @_streamed
@@ -643,34 +639,14 @@ def svm_adamw(params, grads, m, v, step: int, lr: float, *, beta1: float = 0.9, 
     on the gradients, a number or a one-element float32 device tensor (clipping by a norm known on the device)."""
     lib = load()
     count = len(params)
-    decay = [weight_decay] * count if not isinstance(weight_decay, (list, tuple)) else weight_decay
-    for name, lst in (("grads", grads), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale), ("master", master),
-                      ("weight_decay", decay)):
-        if lst is not None and len(lst) != count:
-            raise ValueError(f"{name} must have one entry for each of the {count} params")
     device = torch.cuda.current_device()
-    tensors = (svm_adamw_tensor * count)()
-    for i, p in enumerate(params):
-        n = p.numel()
-        t = tensors[i]
-        t.param = _flat(p, _FLOATS, n, device, "params")
-        t.grad = _flat(grads[i], _FLOATS, n, device, "grads")
-        t.m = _flat(m[i], _STATES, n, device, "m")
-        t.v = _flat(v[i], (m[i].dtype,), n, device, "v")
-        if m[i].dtype != torch.float32:
-            if m_scale is None or v_scale is None:
-                raise ValueError("float8 states need m_scale and v_scale")
-            blocks = -(-n // ADAMW_BLOCK)
-            t.m_scale = _flat(m_scale[i], _F32_ONLY, blocks, device, "m_scale")
-            t.v_scale = _flat(v_scale[i], _F32_ONLY, blocks, device, "v_scale")
-            t.state_type = SVM_F8
-        if master is not None and master[i] is not None:
-            t.master = _flat(master[i], _F32_ONLY, n, device, "master")
-        t.count, t.weight_decay, t.param_type, t.grad_type = n, decay[i], _FLOATS[p.dtype], _FLOATS[grads[i].dtype]
+    tensors = _describe(params, grads, m, v, m_scale, v_scale, master, weight_decay, device, ADAMW_BLOCK)
     a = svm_adamw_params(struct_size=C.sizeof(svm_adamw_params), step=step, lr=lr, beta1=beta1, beta2=beta2, eps=eps,
                          grad_scale=1.0)
     if isinstance(grad_scale, torch.Tensor):
-        a.grad_scale_device = _flat(grad_scale, _F32_ONLY, 1, device, "grad_scale")
+        if grad_scale.get_device() != device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
+            raise TypeError("grad_scale must be a number or a one-element float32 tensor on the current device")
+        a.grad_scale_device = grad_scale.data_ptr()
     else:
         a.grad_scale = grad_scale
     _check(lib.svm_adamw(tensors, count, C.byref(a), _stream_options(device)))

@@ -1,0 +1,80 @@
+"""The checks of an AdamW step's lists (csrc/tensor_list.cpp): what is refused, and what the C array then holds."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2311_14908_amd import svmx
+
+F8 = torch.float8_e4m3fn
+
+
+def describe(p, g=None, m=None, v=None, ms=None, vs=None, master=None, decay=0.0, device=0):
+    return svmx._describe(p, p if g is None else g, p if m is None else m, p if v is None else v, ms, vs, master, decay, device, 256)
+
+
+@pytest.mark.parametrize("bad", [
+    lambda t: describe([t]),  # not on a GPU
+    lambda t: describe([1.0]),
+    lambda t: describe([None]),
+    lambda t: describe(3),
+    lambda t: describe([t], g=[]),
+    lambda t: describe([t], m=[t, t]),
+    lambda t: describe([t], v=None, g=None, m=None, ms=[t, t]),
+    lambda t: describe([t], master=[]),
+    lambda t: describe([t], decay=[0.1, 0.2]),
+    lambda t: describe([t], decay="much"),
+    lambda t: describe([t], decay=[None]),
+    lambda t: svmx._describe([t], [t]),
+    lambda t: svmx._describe([t], None, None, None, None, None, None, 0.0, 0, 256),
+])
+def test_refusals(bad):
+    with pytest.raises((TypeError, ValueError)):
+        bad(torch.zeros(4))
+
+
+def test_nothing():
+    assert describe([]) == b"" and describe((), (), (), ()) == b"" and describe([], decay=[]) == b""
+
+
+@pytest.mark.gpu
+def test_what_the_array_holds():
+    sizes = [5, 0, 256, 257]
+    p = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in sizes]
+    g = [torch.zeros(s, dtype=torch.float16, device="cuda") for s in sizes]
+    m, v, ms, vs = svmx.svm_adamw_states(p, F8)
+    m[0], v[0] = torch.zeros(5, device="cuda"), torch.zeros(5, device="cuda")  # one entry with fp32 states
+    master = [None, None, torch.zeros(256, device="cuda"), None]
+    decay = [0.1, 0.2, 0.3, 0.4]
+    raw = describe(p, tuple(g), m, v, ms, vs, master, decay, torch.cuda.current_device())
+    got = (svmx.svm_adamw_tensor * 4).from_buffer_copy(raw)
+    for i, t in enumerate(got):
+        f8 = i > 0
+        assert (t.param or 0, t.grad or 0, t.m or 0, t.v or 0) == (p[i].data_ptr(), g[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr())
+        assert (t.m_scale or 0, t.v_scale or 0) == ((ms[i].data_ptr(), vs[i].data_ptr()) if f8 else (0, 0))
+        assert (t.master or 0) == (master[i].data_ptr() if master[i] is not None else 0)
+        assert (t.count, t.weight_decay, t.reserved) == (sizes[i], decay[i], 0)
+        assert (t.param_type, t.grad_type, t.state_type) == (svmx.SVM_BF16, svmx.SVM_F16, svmx.SVM_F8 if f8 else svmx.SVM_F32)
+    assert C.sizeof(got) == len(raw)
+
+
+@pytest.mark.gpu
+def test_refusals_on_the_device():
+    t = torch.zeros(300, device="cuda")
+    m8, s = torch.zeros(300, dtype=torch.uint8, device="cuda").view(F8), torch.zeros(2, device="cuda")
+    here = torch.cuda.current_device()
+    describe([t], device=here)
+    describe([t], m=[m8], v=[m8], ms=[s], vs=[s], device=here)
+    for bad in (lambda: describe([t], device=here + 1), lambda: describe([t.double()], device=here),
+                lambda: describe([t], g=[t[::2]], device=here), lambda: describe([t], g=[t[:299]], device=here),
+                lambda: describe([t], m=[m8], device=here), lambda: describe([t], m=[m8], v=[m8], device=here),
+                lambda: describe([t], m=[m8], v=[m8], ms=[s], device=here),
+                lambda: describe([t], m=[m8], v=[m8], ms=[s], vs=[s[:1]], device=here),
+                lambda: describe([t], m=[m8], v=[m8], ms=[s], vs=[s.half()], device=here),
+                lambda: describe([t], m=[t.half()], device=here), lambda: describe([m8], g=[t], m=[t], v=[t], device=here),
+                lambda: describe([t], master=[t.half()], device=here), lambda: describe([t], master=[t.cpu()], device=here),
+                lambda: describe([torch.zeros(4, 6, device="cuda").t()], device=here)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    with pytest.raises(TypeError):
+        svmx.svm_adamw([t], [t], [t], [t], 1, 1e-3, grad_scale=torch.ones(2, device="cuda"))
